@@ -381,6 +381,93 @@ int pc_parallel_attn_static(const void* q, const void* kc, const void* vc, const
                             void* stream);
 size_t pc_parallel_attn_static_max_bytes(void);   /* = PC_STATIC_SCRATCH_BYTES */
 
+/* ---- many answers over one compressed document (extension) -----------------------------------
+ * Serving: the compressed segments of a document are a prefix that many sequences share (several
+ * questions, sampled answers, drafted tokens); each sequence adds a tail of its own.
+ *
+ * Rows of keys and values [n, n_seg, H_kv, cap, D], as the gather leaves them (n = batch).  bf16 with
+ * both scales NULL; or 8-bit rows: OCP E4M3 codes (one byte a value) with one fp32 scale a row,
+ * value = code * scale, as pc_kv_append_row8 writes them. */
+typedef struct pc_row_cache {
+  const void*    k;                /* keys, already rotated; 16-byte aligned                          */
+  const void*    v;
+  const float*   k_scale;          /* [n, n_seg, H_kv, cap] fp32, both or neither                     */
+  const float*   v_scale;
+  const int32_t* seg_len;          /* valid rows (device), clamped to [0, cap]; NULL => cap:          */
+  int32_t        seg_len_per_head; /*   [n, n_seg] if 0, [n, n_seg, H_kv] if 1                        */
+  int32_t        n_seg;
+  int32_t        cap;
+} pc_row_cache;
+
+/* Attention of a batch over shared prefixes: n_prefix prefixes, batch = n_prefix * F sequences, sequence b
+ * reads prefix b / F, and its own tail, under one softmax:
+ *   out[b, t, h, :] = softmax over { prefix[b / F, s, g, j] for all s, j < seg_len }
+ *                                U { tail[b, g, j], j < visible } of q . k * scale, times the values
+ * A key of a prefix is read from memory once for the query rows of all F sequences.
+ *   q [B, n_q, H_q, D] bf16; q_pos [B] int32 (device), nullable: row t is rotated here at position
+ *     pos0 + q_pos[b] + t >= 0 (rounded to bf16 once), so that the tails' lengths in front of the step serve
+ *     as q_pos, with pos0 the position of a tail's first row; NULL: q arrives rotated.
+ *   prefix: rows of n = n_prefix; NULL for none.   tail: rows of n = batch with n_seg = 1; NULL for none.
+ *   tail_own: 0: every tail row is visible to every query row.  1: the tail's last n_q rows are the query rows'
+ *     own: row t sees tail rows j < seg_len - (n_q - 1 - t) (append the rows first, then call).
+ *   out [B, n_q, H_q, D] bf16; a row that sees no key is 0.   lse_out [B, H_q, n_q] fp32, nullable (natural log;
+ *     -inf where no key is seen).
+ * Whatever lies in rows behind the lengths, and in rows that a query row does not see, stays out of its result,
+ * infinities and NaN included.
+ * Arithmetic: bf16 MFMA products (8-bit codes widened exactly), logits scaled in fp32, fp32 softmax and
+ * accumulation, probabilities (times the row's V scale) rounded to bf16 for the second product.
+ * batch, n_q, n_seg, H_q up to 2^20 each, cap up to 2^24, B n_q H_q < 2^25; PC_ERR_SHAPE otherwise.
+ * Workspace: pc_shared_attn_workspace_bytes(...) of the same sizes and formats. */
+int pc_shared_attn(const void* q, const int32_t* q_pos, int32_t pos0, float rope_base, float softmax_scale,
+                   const pc_row_cache* prefix, const pc_row_cache* tail, int32_t tail_own, int32_t batch,
+                   int32_t n_prefix, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                   void* out, float* lse_out, void* ws, size_t ws_bytes, void* stream);
+size_t pc_shared_attn_workspace_bytes(const pc_row_cache* prefix, const pc_row_cache* tail, int32_t batch,
+                                      int32_t n_prefix, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads,
+                                      int32_t head_dim);
+
+/* Quantise keys and values as they are written: n_new rows a sequence into 8-bit rows of one segment, behind
+ * the len_in[b] rows it holds.
+ *   scale = max over the row of |x| / 448 (1 if that is 0; at least 2^-126), code = E4M3(x / scale), fp32
+ *   division, to nearest, ties to the even code.  Keys are rotated first (pos != NULL: row t at position
+ *   pos0 + pos[b] + t >= 0) and rounded only once, to the code.  A row that holds an infinity or a NaN reads back as NaN.
+ *   k_new, v_new [B, n_new, H_kv, D] bf16;  pos [B] int32 (device), nullable
+ *   k8, v8 [B, H_kv, cap, D] uint8, k_scale, v_scale [B, H_kv, cap] fp32 in/out
+ *   len_in [B] int32 (device), nullable (all 0); len_out [B], nullable: min(len_in + n_new, cap).  They must not
+ *   overlap: the rows of a sequence are written by many workgroups, each of which reads len_in.
+ * Rows that do not fit are dropped.  A compacted cache [S, H_kv, k_t, D] of the gather is quantised by one call
+ * with batch = S * H_kv, n_new = cap = k_t, one KV head.  No workspace. */
+int pc_kv_append_row8(const void* k_new, const void* v_new, const int32_t* pos, int32_t pos0, float rope_base, int32_t batch,
+                      int32_t n_new, int32_t cap, int32_t n_kv_heads, int32_t head_dim, void* k8, void* v8,
+                      float* k_scale, float* v_scale, const int32_t* len_in, int32_t* len_out, void* stream);
+/* Read 8-bit rows back: k, v [B, H_kv, cap, D] bf16 = code * scale, rounded once.  Rows behind seg_len [B]
+ * (device, nullable: all cap) are not written.  No workspace. */
+int pc_kv_read_row8(const void* k8, const void* v8, const float* k_scale, const float* v_scale,
+                    const int32_t* seg_len, int32_t batch, int32_t cap, int32_t n_kv_heads, int32_t head_dim,
+                    void* k, void* v, void* stream);
+
+/* Verify drafted tokens against the target's probabilities, from given random numbers.
+ *   draft [B, n_draft] int32 tokens; draft_len [B] int32 (device), nullable: the first draft_len[b] of them
+ *     count (clamped to [0, n_draft])
+ *   draft_prob [B, n_draft, V] fp32: the distributions they were drawn from; NULL: they were not drawn (a
+ *     point mass on each)
+ *   target_prob [B, n_draft + 1, V] fp32;  u [B, n_draft] fp32 uniform in [0, 1);  noise [B, V] fp32, drawn
+ *     from the exponential distribution of mean 1
+ * Draft i stands iff u_i * draft_prob_i(d_i) < target_prob_i(d_i) and every draft before it stands (a token
+ * outside [0, V) never does).  With a standing, the next token is drawn from max(target_prob_a - draft_prob_a, 0) where
+ * draft a fell (target_prob_a itself if that is 0 throughout), from target_prob_a where none did: the v of largest
+ * r(v) / noise(v) among r(v) > 0, the lowest at ties; -1 if there is none.  Each step is one fp32 operation an
+ * entry (the quotient correctly rounded): results do not depend on the order of the work.
+ *   tokens [B, n_draft + 1] int32 out: the standing drafts, the next token, then -1;  n_accepted [B] int32 out
+ *   len_in, len_out [B] int32 (device), both or neither: len_out = len_in + 1 + n_accepted, the rows of a cache
+ *     that stand (the last token's and the standing drafts' behind len_in); may be the same array.
+ * Workspace: pc_verify_drafts_workspace_bytes(batch, n_draft, vocab). */
+int pc_verify_drafts(const int32_t* draft, const int32_t* draft_len, const float* draft_prob,
+                     const float* target_prob, const float* u, const float* noise, int32_t batch,
+                     int32_t n_draft, int32_t vocab, int32_t* tokens, int32_t* n_accepted,
+                     const int32_t* len_in, int32_t* len_out, void* ws, size_t ws_bytes, void* stream);
+size_t pc_verify_drafts_workspace_bytes(int32_t batch, int32_t n_draft, int32_t vocab);
+
 /* ---- housekeeping -------------------------------------------------------------------------- */
 const char* pc_status_string(int status);   /* static string, never NULL                       */
 int         pc_last_hip_error(void);        /* hipError_t of the last PC_ERR_HIP on this thread */

@@ -27,6 +27,8 @@ SYMBOLS = [
     "pc_chunk_queue_update", "pc_gather_kv_amax", "pc_kv_quantize_fp8_amax",
     "pc_copy_ceiling", "pc_decode_step", "pc_decode_step_workspace_bytes", "pc_decode_step_fp8",
     "pc_decode_step_fp8_workspace_bytes", "pc_layer_forward", "pc_layer_workspace_bytes",
+    "pc_shared_attn", "pc_shared_attn_workspace_bytes", "pc_kv_append_row8", "pc_kv_read_row8",
+    "pc_verify_drafts", "pc_verify_drafts_workspace_bytes",
 ]
 
 
@@ -34,6 +36,11 @@ class pc_shape(Structure):
     _fields_ = [("n_chunks", c_int32), ("chunk_len", c_int32), ("query_len", c_int32),
                 ("n_q_heads", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32),
                 ("obs_window", c_int32), ("rope_base", c_float), ("softmax_scale", c_float)]
+
+
+class pc_row_cache(Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p), ("seg_len", c_void_p),
+                ("seg_len_per_head", c_int32), ("n_seg", c_int32), ("cap", c_int32)]
 
 
 class PcError(RuntimeError):
@@ -127,6 +134,19 @@ def lib():
     L.pc_layer_forward.restype = c_int
     L.pc_layer_workspace_bytes.argtypes = [POINTER(pc_shape), c_int32, c_int32]
     L.pc_layer_workspace_bytes.restype = c_size_t
+    L.pc_shared_attn.argtypes = ([P, P, c_int32, c_float, c_float, POINTER(pc_row_cache), POINTER(pc_row_cache)] + [c_int32] * 7 +
+                                 [P, P, P, c_size_t, P])
+    L.pc_shared_attn.restype = c_int
+    L.pc_shared_attn_workspace_bytes.argtypes = [POINTER(pc_row_cache), POINTER(pc_row_cache)] + [c_int32] * 6
+    L.pc_shared_attn_workspace_bytes.restype = c_size_t
+    L.pc_kv_append_row8.argtypes = [P, P, P, c_int32, c_float] + [c_int32] * 5 + [P] * 7
+    L.pc_kv_append_row8.restype = c_int
+    L.pc_kv_read_row8.argtypes = [P] * 5 + [c_int32] * 4 + [P] * 3
+    L.pc_kv_read_row8.restype = c_int
+    L.pc_verify_drafts.argtypes = [P] * 6 + [c_int32] * 3 + [P] * 5 + [c_size_t, P]
+    L.pc_verify_drafts.restype = c_int
+    L.pc_verify_drafts_workspace_bytes.argtypes = [c_int32] * 3
+    L.pc_verify_drafts_workspace_bytes.restype = c_size_t
     _lib = L
     return L
 
@@ -348,6 +368,75 @@ def pc_parallel_attn_fp8(q, k8, v8, k_scale, v_scale, seg_len, k_tail, v_tail, t
                                       n_seg, k_t, n_q_heads,
                                       n_kv_heads, head_dim, q_pos0, rope_base, softmax_scale,
                                       _ptr(out), _ptr(lse_out), p, n, _stream()), "pc_parallel_attn_fp8")
+
+
+def make_row_cache(k, v, k_scale=None, v_scale=None, seg_len=None, seg_len_per_head=0):
+    """Rows of keys and values [n, n_seg, H_kv, cap, D] for pc_shared_attn: bf16, or uint8 codes with the scales
+    [n, n_seg, H_kv, cap]; the tensors are kept alive with it."""
+    if k.dim() != 5 or k.shape != v.shape or k.dtype != v.dtype:
+        raise ValueError("k and v must be [n, n_seg, n_kv_heads, cap, head_dim] and of one type")
+    if k.dtype != (torch.bfloat16 if k_scale is None else torch.uint8) or (k_scale is None) != (v_scale is None):
+        raise ValueError("rows are bfloat16 without scales, or uint8 codes with both scales")
+    for s in (k_scale, v_scale):
+        if s is not None and (s.dtype != torch.float32 or s.shape != k.shape[:4]):
+            raise ValueError("scales must be float32 [n, n_seg, n_kv_heads, cap]")
+    want = k.shape[:3] if seg_len_per_head else k.shape[:2]
+    if seg_len is not None and (seg_len.dtype != torch.int32 or seg_len.numel() != want.numel()):
+        raise ValueError("seg_len must be int32, a length a segment (and head with seg_len_per_head)")
+    c = pc_row_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(seg_len), int(bool(seg_len_per_head)),
+                     k.shape[1], k.shape[3])
+    c.tensors = (k, v, k_scale, v_scale, seg_len)
+    return c
+
+
+def _rows_ref(c):
+    return None if c is None else ctypes.byref(c)
+
+
+def _rows_fit(c, n, n_kv_heads, head_dim, where):
+    shape = c.tensors[0].shape if c is not None else None
+    if shape is not None and (shape[0], shape[2], shape[4]) != (n, n_kv_heads, head_dim):
+        raise ValueError(f"{where}: rows of {tuple(shape)} are not [{n}, n_seg, {n_kv_heads}, cap, {head_dim}]")
+
+
+def pc_shared_attn_workspace_bytes(prefix, tail, batch, n_prefix, n_q, n_q_heads, n_kv_heads, head_dim):
+    return int(lib().pc_shared_attn_workspace_bytes(_rows_ref(prefix), _rows_ref(tail), batch, n_prefix, n_q, n_q_heads,
+                                                    n_kv_heads, head_dim))
+
+
+def pc_shared_attn(q, prefix, tail, batch, n_prefix, n_q, n_q_heads, n_kv_heads, head_dim, out, lse_out, ws, q_pos=None,
+                   pos0=0, rope_base=0.0, softmax_scale=0.0, tail_own=0):
+    """prefix, tail: from make_row_cache, or None."""
+    _rows_fit(prefix, n_prefix, n_kv_heads, head_dim, "prefix")
+    _rows_fit(tail, batch, n_kv_heads, head_dim, "tail")
+    p, n = _ws(ws)
+    _check(lib().pc_shared_attn(_ptr(q), _ptr(q_pos), pos0, rope_base, softmax_scale, _rows_ref(prefix), _rows_ref(tail),
+                                int(bool(tail_own)), batch, n_prefix, n_q, n_q_heads, n_kv_heads, head_dim, _ptr(out),
+                                _ptr(lse_out), p, n, _stream()), "pc_shared_attn")
+
+
+def pc_kv_append_row8(k_new, v_new, batch, n_new, cap, n_kv_heads, head_dim, k8, v8, k_scale, v_scale, len_in, len_out,
+                      pos=None, pos0=0, rope_base=0.0):
+    _check(lib().pc_kv_append_row8(_ptr(k_new), _ptr(v_new), _ptr(pos), pos0, rope_base, batch, n_new, cap, n_kv_heads, head_dim,
+                                   _ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), _ptr(len_in), _ptr(len_out),
+                                   _stream()), "pc_kv_append_row8")
+
+
+def pc_kv_read_row8(k8, v8, k_scale, v_scale, seg_len, batch, cap, n_kv_heads, head_dim, k, v):
+    _check(lib().pc_kv_read_row8(_ptr(k8), _ptr(v8), _ptr(k_scale), _ptr(v_scale), _ptr(seg_len), batch, cap, n_kv_heads,
+                                 head_dim, _ptr(k), _ptr(v), _stream()), "pc_kv_read_row8")
+
+
+def pc_verify_drafts_workspace_bytes(batch, n_draft, vocab):
+    return int(lib().pc_verify_drafts_workspace_bytes(batch, n_draft, vocab))
+
+
+def pc_verify_drafts(draft, draft_prob, target_prob, u, noise, batch, n_draft, vocab, tokens, n_accepted, ws,
+                     draft_len=None, len_in=None, len_out=None):
+    p, n = _ws(ws)
+    _check(lib().pc_verify_drafts(_ptr(draft), _ptr(draft_len), _ptr(draft_prob), _ptr(target_prob), _ptr(u), _ptr(noise),
+                                  batch, n_draft, vocab, _ptr(tokens), _ptr(n_accepted), _ptr(len_in), _ptr(len_out),
+                                  p, n, _stream()), "pc_verify_drafts")
 
 
 def pc_profile_begin(kernel=None):

@@ -270,3 +270,83 @@ class DecodeCacheFp8:
                              self.k_tail, self.v_tail, self.tail_len, self.cap, self.B, self.S, self.kt, self.Hq,
                              self.Hkv, self.D, pos, self.rope_base, self.scale, self.out, self.lse, self.ws)
         return self.out
+
+
+class SharedPrefixDecoder:
+    """Many answers over few compressed documents: n_prefix documents' compacted segments, each shared by batch /
+    n_prefix sequences (sequence b reads document b // (batch // n_prefix)), and a tail a sequence that starts as its
+    query block's keys / values and grows as tokens are generated, kept in 8-bit rows that are rounded as they are
+    written.  With eight_bit_prefix the segments are kept so too.
+
+    A step is append -> attention (-> the caller's remaining layers -> verification of drafted tokens):
+      step(q, k, v)   the n rows a sequence (its last token and the drafts behind it) of this layer
+      accept()        all n rows stand (no drafts), or
+      verify(...)     those up to the first draft that falls stand; the others' rows are written over by the next step.
+    Lengths live on the device, so a run of steps is a run of library calls with no host round trip."""
+
+    def __init__(self, batch, n_prefix, n_seg, keep_tokens, tail_cap, n_q_heads, n_kv_heads, head_dim, rope_base,
+                 tail_pos, max_rows=1, softmax_scale=0.0, eight_bit_prefix=False, device="cuda"):
+        self.B, self.P, self.S, self.kt, self.cap = batch, n_prefix, n_seg, keep_tokens, tail_cap
+        self.Hq, self.Hkv, self.D = n_q_heads, n_kv_heads, head_dim
+        self.rope_base, self.scale, self.pos0, self.max_rows = rope_base, softmax_scale, tail_pos, max_rows
+        i32, f32 = torch.int32, torch.float32
+        rows8 = lambda *shape: [torch.zeros((*shape, head_dim), dtype=torch.uint8, device=device) for _ in "kv"] + \
+            [torch.ones(shape, dtype=f32, device=device) for _ in "kv"]
+        self.eight_bit_prefix = eight_bit_prefix
+        seg = (n_prefix, n_seg, n_kv_heads, keep_tokens)
+        if eight_bit_prefix:
+            self.prefix = rows8(*seg)
+        else:
+            self.prefix = [torch.zeros((*seg, head_dim), dtype=torch.bfloat16, device=device) for _ in "kv"]
+        self.tail = rows8(batch, 1, n_kv_heads, tail_cap)
+        self.len = torch.zeros((batch,), dtype=i32, device=device)          # rows of the tails that stand
+        self.len_new = torch.zeros_like(self.len)                           # with those of the step at hand
+        self.prefix_rows = None
+        self.lse = torch.empty((batch, n_q_heads, max_rows), dtype=f32, device=device)
+        self.out = torch.empty((batch, max_rows, n_q_heads, head_dim), dtype=torch.bfloat16, device=device)
+        self.ws = None
+
+    def load(self, kc, vc, seg_len=None, seg_len_per_head=0, k_tail=None, v_tail=None):
+        """kc, vc [n_prefix, n_seg, H_kv, k_t, D] bf16 compacted segments (copied, or rounded to 8-bit rows), seg_len
+        int32 or None (all k_t); k_tail, v_tail [B, n0, H_kv, D] rotated keys / values of the query blocks."""
+        if self.eight_bit_prefix:                                           # a segment's head is a sequence of its own
+            k8, v8, ks, vs = self.prefix
+            B.pc_kv_append_row8(kc, vc, self.P * self.S * self.Hkv, self.kt, self.kt, 1, self.D, k8, v8, ks, vs, None, None)
+        else:
+            self.prefix[0].copy_(kc); self.prefix[1].copy_(vc)
+        self.prefix_rows = B.make_row_cache(*self.prefix, seg_len=seg_len, seg_len_per_head=seg_len_per_head)
+        self.ws = None
+        self.len.zero_()
+        if k_tail is not None:
+            self._append(k_tail, v_tail, None)
+            self.accept()
+
+    def _append(self, k, v, pos):
+        k8, v8, ks, vs = self.tail
+        B.pc_kv_append_row8(k, v, self.B, k.shape[1], self.cap, self.Hkv, self.D, k8, v8, ks, vs, self.len, self.len_new,
+                            pos=pos, pos0=self.pos0, rope_base=self.rope_base)
+
+    def step(self, q, k, v):
+        """q [B, n, H_q, D], k, v [B, n, H_kv, D] before RoPE, n <= max_rows: rows at positions tail_pos + len .. of
+        their sequences.  Returns out [B, n, H_q, D] (a view of the step's buffer)."""
+        n = q.shape[1]
+        self._append(k, v, self.len)
+        tail = B.make_row_cache(*self.tail, seg_len=self.len_new)
+        if self.ws is None:
+            self.ws = B.alloc_workspace(max(B.pc_shared_attn_workspace_bytes(self.prefix_rows, tail, self.B, self.P, m, self.Hq,
+                                                                             self.Hkv, self.D)
+                                            for m in range(1, self.max_rows + 1)), q.device)
+        out = self.out.view(-1)[:q.numel()].view(q.shape)
+        lse = self.lse.view(-1)[:self.B * self.Hq * n].view(self.B, self.Hq, n)
+        B.pc_shared_attn(q, self.prefix_rows, tail, self.B, self.P, n, self.Hq, self.Hkv, self.D, out, lse, self.ws,
+                         q_pos=self.len, pos0=self.pos0, rope_base=self.rope_base, softmax_scale=self.scale, tail_own=1)
+        return out
+
+    def accept(self):
+        """Every row of the step stands."""
+        self.len, self.len_new = self.len_new, self.len
+
+    def verify(self, draft, draft_prob, target_prob, u, noise, tokens, n_accepted, ws, draft_len=None):
+        """pc_verify_drafts; the rows of the last token and of the standing drafts stay in the tails."""
+        B.pc_verify_drafts(draft, draft_prob, target_prob, u, noise, self.B, draft.shape[1], target_prob.shape[2], tokens,
+                           n_accepted, ws, draft_len=draft_len, len_in=self.len, len_out=self.len)
