@@ -386,8 +386,8 @@ __device__ __forceinline__ int pc_wave_scan(int x) {
 __device__ __forceinline__ int pc_first_lens(const PcSegLens& L, int lane) {
   return L.seg_len && L.n_seg > 0 ? L.seg_len[L.at(min(lane, L.n_seg - 1))] : 0;
 }
-__device__ __forceinline__ PcBlockCursor pc_blocks_begin(const PcSegLens& L, int part, int n_parts, PcDiv parts_div, int wave, int lane, int first) {
-  constexpr int WAVES = 4;
+template <int WAVES = 4>
+__device__ __forceinline__ PcBlockCursor pc_blocks_begin(const PcSegLens& L, int part, int n_parts, PcDiv parts_div, int wave, int lane, int first, int waves = WAVES) {
   PcBlockCursor c; c.s = 0; c.blk = 0; c.n_blk = 0; c.len = 0; c.left = 0;
   const int nb_full = (L.k_t + 31) / 32;
   // lanes take a segment each, 64 segments per round; up to 64 segments the one round is kept
@@ -406,7 +406,7 @@ __device__ __forceinline__ PcBlockCursor pc_blocks_begin(const PcSegLens& L, int
   }
   const int per = pc_div(total, parts_div), extra = total - per * n_parts;
   const int lo = part * per + min(part, extra), n = per + (part < extra);
-  const int w_lo = lo + n * wave / WAVES, w_hi = lo + n * (wave + 1) / WAVES;
+  const int w_lo = lo + n * wave / waves, w_hi = lo + n * (wave + 1) / waves;
   if (w_lo >= w_hi) return c;
   c.left = w_hi - w_lo;
   if (!L.seg_len) {

@@ -48,12 +48,14 @@ struct PcSharedCall {
   void* out;               // [B, n_q, H_q, D]
   float* lse;              // [B, H_q, n_q] or nullptr
 };
-// How the keys are cut: partial results a query row from the prefix's keys and from the tail's
-struct PcSharedSplit { int prefix_parts, tail_parts; };
-PcSharedSplit pc_shared_split(const PcSharedCall& c);
-bool pc_shared_fits(const PcSharedCall& c);
-size_t pc_shared_ws_bytes(const PcSharedCall& c);
-int pc_launch_shared_attn(const PcSharedCall& c, void* ws, hipStream_t st);
+// How a call is done: alone, one launch; else the sides' partials (the tails' of up to 16 rows behind the prefix's, in
+// their launch) and the merge.  A side: groups (caches x KV heads x tiles) of workgroups, `parts` runs of keys each.
+struct PcSharedSide { int body, parts, waves; long long tiles, caches_heads, runs; };      // body 0: no such side; waves: of a run behind the prefix's
+struct PcSharedPlan { PcSharedSide prefix, tail; bool alone; };
+PcSharedPlan pc_shared_plan(const PcSharedCall& c);
+bool pc_shared_fits(const PcSharedCall& c, const PcSharedPlan& p);
+size_t pc_shared_ws_bytes(const PcSharedCall& c, const PcSharedPlan& p);
+int pc_launch_shared_attn(const PcSharedCall& c, const PcSharedPlan& p, void* ws, hipStream_t st);
 
 // ---- 8-bit rows
 int pc_launch_append_row8(const void* k_new, const void* v_new, const int32_t* pos, int pos0, float base, int batch, int n_new,

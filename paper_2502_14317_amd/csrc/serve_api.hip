@@ -15,7 +15,7 @@ static int check_heads(int n_q_heads, int n_kv_heads, int head_dim) {
 
 // Sizes of a shared-prefix call.  The kernels number workgroups, rows and (segment, head) pairs with 32-bit integers.
 static int check_shared_sizes(const pc_row_cache* prefix, const pc_row_cache* tail, int batch, int n_prefix, int n_q,
-                              int n_q_heads, int n_kv_heads, int head_dim, PcSharedCall& c) {
+                              int n_q_heads, int n_kv_heads, int head_dim, PcSharedCall& c, PcSharedPlan& plan) {
   if (batch < 1 || n_prefix < 1 || n_q < 1 || batch > kMost || n_q > kMost || batch % n_prefix != 0) return PC_ERR_SHAPE;
   const int rc = check_heads(n_q_heads, n_kv_heads, head_dim);
   if (rc != PC_OK) return rc;
@@ -36,15 +36,17 @@ static int check_shared_sizes(const pc_row_cache* prefix, const pc_row_cache* ta
   if ((long long)c.prefix.n_seg * ((c.prefix.cap + 31) / 32) > 0x7fffffffLL) return PC_ERR_SHAPE;
   c.batch = batch; c.n_prefix = n_prefix; c.n_q = n_q; c.n_q_heads = n_q_heads; c.n_kv_heads = n_kv_heads;
   c.head_dim = head_dim;
-  return pc_shared_fits(c) ? PC_OK : PC_ERR_SHAPE;
+  plan = pc_shared_plan(c);
+  return pc_shared_fits(c, plan) ? PC_OK : PC_ERR_SHAPE;
 }
 
 extern "C" size_t pc_shared_attn_workspace_bytes(const pc_row_cache* prefix, const pc_row_cache* tail, int32_t batch,
                                                  int32_t n_prefix, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads,
                                                  int32_t head_dim) {
   PcSharedCall c;
-  if (check_shared_sizes(prefix, tail, batch, n_prefix, n_q, n_q_heads, n_kv_heads, head_dim, c) != PC_OK) return 0;
-  return pc_shared_ws_bytes(c);
+  PcSharedPlan plan;
+  if (check_shared_sizes(prefix, tail, batch, n_prefix, n_q, n_q_heads, n_kv_heads, head_dim, c, plan) != PC_OK) return 0;
+  return pc_shared_ws_bytes(c, plan);
 }
 
 extern "C" int pc_shared_attn(const void* q, const int32_t* q_pos, int32_t pos0, float rope_base, float softmax_scale,
@@ -52,7 +54,8 @@ extern "C" int pc_shared_attn(const void* q, const int32_t* q_pos, int32_t pos0,
                               int32_t n_prefix, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
                               void* out, float* lse_out, void* ws, size_t ws_bytes, void* stream) {
   PcSharedCall c;
-  int rc = check_shared_sizes(prefix, tail, batch, n_prefix, n_q, n_q_heads, n_kv_heads, head_dim, c);
+  PcSharedPlan plan;
+  int rc = check_shared_sizes(prefix, tail, batch, n_prefix, n_q, n_q_heads, n_kv_heads, head_dim, c, plan);
   if (rc != PC_OK) return rc;
   if (!q || !out) return PC_ERR_NULL;
   for (const PcRows* r : {&c.prefix, &c.tail}) {
@@ -68,11 +71,11 @@ extern "C" int pc_shared_attn(const void* q, const int32_t* q_pos, int32_t pos0,
   if (!(softmax_scale >= 0.0f) || !isfinite(softmax_scale)) return PC_ERR_SHAPE;
   if ((rc = check_rope(q_pos, rope_base)) != PC_OK) return rc;
   if (!pc_aligned(q, 16) || !pc_aligned(out, 16) || !pc_aligned(q_pos, 4) || !pc_aligned(lse_out, 4)) return PC_ERR_SHAPE;
-  if (!ws || !pc_aligned(ws, 256) || ws_bytes < pc_shared_ws_bytes(c)) return PC_ERR_WORKSPACE;
+  if (!ws || !pc_aligned(ws, 256) || ws_bytes < pc_shared_ws_bytes(c, plan)) return PC_ERR_WORKSPACE;
   c.q = q; c.q_pos = q_pos; c.pos0 = pos0; c.rope_base = rope_base;
   c.scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)head_dim);
   c.tail_own = tail_own; c.out = out; c.lse = lse_out;
-  return pc_launch_shared_attn(c, ws, (hipStream_t)stream);
+  return pc_launch_shared_attn(c, plan, ws, (hipStream_t)stream);
 }
 
 static int check_row8(int batch, int cap, int n_kv_heads, int head_dim) {
