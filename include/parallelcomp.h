@@ -435,13 +435,13 @@ size_t pc_shared_attn_workspace_bytes(const pc_row_cache* prefix, const pc_row_c
  *   k8, v8 [B, H_kv, cap, D] uint8, k_scale, v_scale [B, H_kv, cap] fp32 in/out
  *   len_in [B] int32 (device), nullable (all 0); len_out [B], nullable: min(len_in + n_new, cap).  They must not
  *   overlap: the rows of a sequence are written by many workgroups, each of which reads len_in.
- * Rows that do not fit are dropped.  A compacted cache [S, H_kv, k_t, D] of the gather is quantised by one call
+ * batch * n_new * H_kv < 2^31.  Rows that do not fit are dropped.  A compacted cache [S, H_kv, k_t, D] of the gather is quantised by one call
  * with batch = S * H_kv, n_new = cap = k_t, one KV head.  No workspace. */
 int pc_kv_append_row8(const void* k_new, const void* v_new, const int32_t* pos, int32_t pos0, float rope_base, int32_t batch,
                       int32_t n_new, int32_t cap, int32_t n_kv_heads, int32_t head_dim, void* k8, void* v8,
                       float* k_scale, float* v_scale, const int32_t* len_in, int32_t* len_out, void* stream);
 /* Read 8-bit rows back: k, v [B, H_kv, cap, D] bf16 = code * scale, rounded once.  Rows behind seg_len [B]
- * (device, nullable: all cap) are not written.  No workspace. */
+ * (device, nullable: all cap) are not written.  batch * H_kv * cap < 2^31.  No workspace. */
 int pc_kv_read_row8(const void* k8, const void* v8, const float* k_scale, const float* v_scale,
                     const int32_t* seg_len, int32_t batch, int32_t cap, int32_t n_kv_heads, int32_t head_dim,
                     void* k, void* v, void* stream);

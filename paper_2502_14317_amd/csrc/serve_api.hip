@@ -89,7 +89,8 @@ extern "C" int pc_kv_append_row8(const void* k_new, const void* v_new, const int
                                  float* k_scale, float* v_scale, const int32_t* len_in, int32_t* len_out, void* stream) {
   int rc = check_row8(batch, cap, n_kv_heads, head_dim);
   if (rc != PC_OK) return rc;
-  if (n_new < 0 || (long long)batch * n_new * n_kv_heads > (1LL << 34)) return PC_ERR_SHAPE;
+  // rows are numbered with 31 bits (check_row8 has bounded the first product)
+  if (n_new < 0 || (long long)batch * n_kv_heads * n_new > 0x7fffffffLL) return PC_ERR_SHAPE;
   if ((rc = check_rope(pos, rope_base)) != PC_OK) return rc;
   if (batch == 0) return PC_OK;
   if (n_new > 0 && (!k_new || !v_new || !k8 || !v8 || !k_scale || !v_scale)) return PC_ERR_NULL;
@@ -108,7 +109,7 @@ extern "C" int pc_kv_read_row8(const void* k8, const void* v8, const float* k_sc
                                void* k, void* v, void* stream) {
   const int rc = check_row8(batch, cap, n_kv_heads, head_dim);
   if (rc != PC_OK) return rc;
-  if ((long long)batch * n_kv_heads * cap > (1LL << 34)) return PC_ERR_SHAPE;
+  if ((long long)batch * n_kv_heads * cap > 0x7fffffffLL) return PC_ERR_SHAPE;
   if (batch == 0) return PC_OK;
   if (!k8 || !v8 || !k_scale || !v_scale || !k || !v) return PC_ERR_NULL;
   if (!pc_aligned(k8, 16) || !pc_aligned(v8, 16) || !pc_aligned(k, 16) || !pc_aligned(v, 16) || !pc_aligned(k_scale, 4) ||
