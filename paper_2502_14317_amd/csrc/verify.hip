@@ -23,9 +23,9 @@ struct VerifyRace {
   float bar;                             // the best quotient, a little less
   __device__ __forceinline__ void clear() { key = 0; bar = 0.f; }
   // A quotient that reaches the best one has r >= best noise (1 - 2^-24): the division is for those alone.  (2^-126: a
-  // product below the normal numbers; one beyond them is above every r.)
+  // product below the normal numbers; one beyond them is above every r; infinite noise times nothing yet: divided.)
   __device__ __forceinline__ void entry(float r, float noise, int v) {
-    if (r > 0.f && r + 0x1p-126f >= bar * noise) {
+    if (r > 0.f && !(r + 0x1p-126f < bar * noise)) {
       const float ratio = r / noise;
       if (ratio >= 0.f) {                // (no NaN, no noise below zero)
         const verify_key k = ((verify_key)(__float_as_uint(ratio) & 0x7fffffffu) << 32) | (uint32_t)~v;
