@@ -6,7 +6,7 @@
 // The rows (sequence, t, head of the group) of one KV head are the columns of S^T = K Q^T, so that a key that has been
 // loaded serves them all.  A workgroup of eight wavefronts takes a CU and a run of keys, and leaves a partial (o, lse) a
 // row, which shared_merge_kernel joins by logsumexp:
-//   few rows   (up to 128): a wavefront has 16 or 32 of them and a part of the run, from memory straight into
+//   few rows   (16, 32 or 64): a wavefront has 16 or 32 of them and a part of the run, from memory straight into
 //              registers, a key read by as many wavefronts as there are groups of 32 rows;
 //   row tiles  (256 rows): a wavefront has 32 rows; tiles of 128 keys go through LDS as matrix operands, widened and
 //              transposed once on the way in, so that every wavefront reads them with 16 consecutive bytes a lane;
@@ -900,9 +900,9 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedMergeArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------ launches
-// What a launch's workgroups are: few rows (16, 32, 64, 128), row tiles of 256 rows; odd numbers: 8-bit rows
-enum SharedBody { SHARED_FEW16 = 2, SHARED_FEW32 = 4, SHARED_FEW64 = 6, SHARED_FEW128 = 8, SHARED_TILE = 10 };
-static constexpr int shared_body_rows(int body) { return 8 << body / 2; }
+// What a launch's workgroups are: few rows (16, 32 or 64 of them), row tiles of 256 rows; odd numbers: 8-bit rows
+enum SharedBody { SHARED_FEW16 = 2, SHARED_FEW32 = 4, SHARED_FEW64 = 6, SHARED_TILE = 8 };
+static constexpr int shared_body_rows(int body) { return body >= SHARED_TILE ? 256 : 8 << body / 2; }
 template <int D, int BODY>
 struct SharedBodyOf {
   static constexpr bool Q8 = BODY % 2, FEW = BODY < SHARED_TILE;
@@ -928,39 +928,48 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_rows_kernel(SharedAr
   if constexpr (B::FEW) shared_few_rows<D, B::NC, B::WR, SHARED_WAVES, B::Q8, OWN>(a, run, tile, *(typename B::FewLds*)lds);
   else shared_row_tiles<D, B::NC, B::Q8, OWN>(a, run, tile, *(SharedTilesLds<D, B::NC>*)lds);
 }
-template <int D, int PREFIX, bool Q8, int WAVES>
-__global__ __launch_bounds__(WAVES * PC_WAVE, 2) void shared_alone_kernel(SharedArgs prefix, SharedArgs tail) {
-  __shared__ SharedFewLds<D, 1, 1, WAVES> sm;
-  shared_alone<D, PREFIX, Q8, WAVES>(prefix, tail, (int)blockIdx.x, sm);
+// Four wavefronts: with eight (128 keys, tails of 64) 8.7 us instead of 7.6 at 8 workgroups, 15.1 instead of 9.5 at 512
+#define SHARED_ALONE 4
+template <int D, int PREFIX, bool Q8>
+__global__ __launch_bounds__(SHARED_ALONE * PC_WAVE, 2) void shared_alone_kernel(SharedArgs prefix, SharedArgs tail) {
+  __shared__ SharedFewLds<D, 1, 1, SHARED_ALONE> sm;
+  shared_alone<D, PREFIX, Q8, SHARED_ALONE>(prefix, tail, (int)blockIdx.x, sm);
 }
 
 // ---- host
-static int body_of(long long rows, bool q8) {
-  return (rows <= 16 ? SHARED_FEW16 : (rows <= 32 ? SHARED_FEW32 : (rows <= 64 ? SHARED_FEW64 : (rows <= 128 ? SHARED_FEW128 : SHARED_TILE)))) + q8;
-}
-
 struct SharedCost { double start, block, bytes, blocks; int most; };      // us of a workgroup, of a 32-key block in it; a block's bytes
-static PcSharedSide side_of(long long n_caches, long long rows, int n_kv_heads, bool q8) {
+static double block_bytes(const PcRows& r, int D) { return 32.0 * (r.k_scale ? 2.0 * D + 8 : 4.0 * D); }
+static double blocks_of(const PcRows& r, double share) { return share * r.n_seg * (double)((r.cap + 31) / 32); }
+static PcSharedSide side_of(long long n_caches, long long rows, int n_kv_heads, int body) {
   PcSharedSide s = {};
-  s.body = body_of(rows, q8); s.parts = 1; s.waves = SHARED_WAVES;
+  s.body = body; s.parts = 1; s.waves = SHARED_WAVES;
   s.tiles = (rows + shared_body_rows(s.body) - 1) / shared_body_rows(s.body);
   s.caches_heads = n_caches * n_kv_heads;
   s.runs = s.caches_heads;
   return s;
 }
-// Measured, one workgroup a CU: 27 GB/s of keys a CU where all of them read, 33 where some do; rows x keys of a block at
-// 2.6 (8-bit rows 2.0, row tiles 4.0) TFLOP/s a CU; queries, partials and latencies 5.5 to 10 us a workgroup
+// Measured, one workgroup a CU: 27 GB/s of keys a CU; or the arithmetic, rows x keys of a block at 1.8 to 3.0 TFLOP/s a CU,
+// or a block's latencies; queries, partials and latencies 5.5 to 10 us a workgroup (64 values a row: 0.6 of that)
 static SharedCost cost_of(const PcSharedSide& s, const PcRows& r, int D, double share) {
+  static const struct { double start, bf16, row8, least; } of[] = {      // us, TFLOP/s, TFLOP/s, us
+      {5.5, 2.6, 2.0, 0.0}, {6.5, 1.8, 3.0, 0.0}, {7.5, 2.5, 2.3, 0.35}, {10.0, 3.0, 2.4, 1.1}};
+  const auto& m = of[s.body / 2 - 1];
   SharedCost c = {};
-  const int rows = shared_body_rows(s.body);
-  c.bytes = 32.0 * (r.k_scale ? 2.0 * D + 8 : 4.0 * D);
-  const double flops = 4.0 * 32 * rows * D;
-  const double memory = c.bytes / 27e3, arithmetic = flops / (s.body >= SHARED_TILE ? 4.0e6 : (r.k_scale ? 2.0e6 : 2.6e6));
-  c.start = rows <= 16 ? 5.5 : (rows <= 64 ? 8.0 : 10.0);
-  c.block = memory > arithmetic ? memory : arithmetic;
-  c.blocks = share * r.n_seg * (double)((r.cap + 31) / 32) + 1.0;
+  c.bytes = block_bytes(r, D);
+  const double memory = c.bytes / 27e3, arithmetic = 4.0 * 32 * shared_body_rows(s.body) * D / ((r.k_scale ? m.row8 : m.bf16) * 1e6);
+  c.start = m.start * (D == 64 ? 0.6 : 1.0);
+  c.block = fmax(fmax(memory, arithmetic), m.least);
+  c.blocks = blocks_of(r, share) + 1.0;
   c.most = c.blocks < 8.0 ? 1 : (c.blocks > 256.0 ? 64 : (int)(c.blocks / 4.0));
   return c;
+}
+// One launch, a workgroup of four wavefronts a (sequence, KV head): prefix keys at 58 GB/s a CU (they are in its L2), the
+// tail's at 28, or a block's latency
+static double alone_us(const PcSharedCall& c) {
+  const double a_cu = (double)c.batch * c.n_kv_heads / 256.0, at_once = a_cu < 1.0 ? 1.0 : a_cu;
+  const double p = blocks_of(c.prefix, 1.0), t = blocks_of(c.tail, 0.75) + 1.0;
+  return 5.7 + 0.7 * a_cu + fmax(at_once * p * block_bytes(c.prefix, c.head_dim) / 58e3, 0.13 * p) +
+         fmax(at_once * t * block_bytes(c.tail, c.head_dim) / 28e3, 0.23 * t);
 }
 // A workgroup of 8 / waves tails' runs: the CU's reads, or a wavefront's blocks one after the other
 static double tails_us(const SharedCost& c, int waves, int tp) {
@@ -978,14 +987,8 @@ static double time_of(double one_p, int np, double one_t, int nt) {
   return us + (t_us > last ? t_us : last);
 }
 static bool tails_behind(const PcSharedPlan& p) { return p.prefix.body && p.tail.body && p.tail.body <= SHARED_FEW16 + 1; }
-PcSharedPlan pc_shared_plan(const PcSharedCall& c) {
-  const int G = c.n_q_heads / c.n_kv_heads;
-  PcSharedPlan p = {};
-  const long long own_rows = (long long)c.n_q * G, keys = (long long)c.prefix.n_seg * c.prefix.cap;
-  p.alone = own_rows <= 16 && keys <= 512 && c.tail.cap <= 1024;
-  if (p.alone) return p;
-  if (c.prefix.n_seg > 0) p.prefix = side_of(c.n_prefix, (long long)(c.batch / c.n_prefix) * own_rows, c.n_kv_heads, c.prefix.k_scale);
-  if (c.tail.n_seg > 0) p.tail = side_of(c.batch, own_rows, c.n_kv_heads, c.tail.k_scale);
+// The cuts of least time for p's bodies; returns that time without the launches'
+static double cut_of(const PcSharedCall& c, PcSharedPlan& p) {
   SharedCost pc = {0, 0, 0, 0, 1}, tc = {0, 0, 0, 0, 1};
   if (p.prefix.body) pc = cost_of(p.prefix, c.prefix, c.head_dim, 1.0);
   if (p.tail.body) tc = cost_of(p.tail, c.tail, c.head_dim, 0.75);
@@ -1003,8 +1006,11 @@ PcSharedPlan pc_shared_plan(const PcSharedCall& c) {
     const long long tails = (tg * tp * waves + SHARED_WAVES - 1) / SHARED_WAVES;
     const int nt = (int)(tails < (1 << 24) ? tails : 1 << 24);
     const double one_t = tg ? (behind ? tails_us(tc, waves, tp) : tc.start + tc.block * tc.blocks / tp) : 0.0;
+    long long weighed = 0;
     auto weigh = [&](long long pp) {
       pp = pp < 1 ? 1 : (pp > pc.most ? pc.most : pp);
+      if (pp == weighed) return;
+      weighed = pp;
       const int np = (int)(pg * pp < (1 << 24) ? pg * pp : 1 << 24);
       const double us = time_of(pc.start + pc.block * pc.blocks / (double)pp, np, one_t, nt) + row_us * (double)((pg ? pp : 0) + (tg ? tp : 0));
       if (least < 0.0 || us < least) {
@@ -1019,9 +1025,41 @@ PcSharedPlan pc_shared_plan(const PcSharedCall& c) {
     for (int fill = 256; fill <= 768; fill += 256)
       for (int part : {0, nt, nt / 2}) weigh((fill - part) / pg);
   }
-  p.prefix.runs = p.prefix.caches_heads * p.prefix.parts;
-  p.tail.runs = p.tail.caches_heads * p.tail.parts;
-  return p;
+  return least;
+}
+// Of the bodies that fit, and of one launch for all (up to 16 rows), the one of least estimated time.  688 calls of 32 to 4096
+// rows a KV head and 512 to 16384 keys (both formats, 64 and 128 values) were timed with each body, and in one launch where
+// that is possible: the choice costs 2 % over the best on average (7 % at the 90th percentile); 64 rows at up to 128 and tiles
+// beyond, by the number of rows alone, cost 13 %; one launch at up to 512 keys, 15 % where it is possible (now 1 %).  us with
+// 32 rows / 64 rows / tiles, bf16: (64 rows x 1024 keys) 13.8 / 16.0 / 18.9, (512 x 1024) 26 / 19.5 / 31, (512 x 16384) 109 / 96
+// / 82, (4096 x 16384) 761 / 606 / 316; 8 bits: (64 x 1024) 13.8 / 15.9 / 20, (512 x 16384) 74 / 77 / 91, (4096 x 16384) 475 /
+// 439 / 412.  One launch / two: (16 sequences, 128 keys, tails of 64) 7.8 / 13.7, (16, 1024, 64) 14.9 / 15.2, (4, 1024, 512) 20 / 14.
+PcSharedPlan pc_shared_plan(const PcSharedCall& c) {
+  const long long own_rows = (long long)c.n_q * (c.n_q_heads / c.n_kv_heads), rows = c.batch / c.n_prefix * own_rows;
+  auto bodies = [](long long n, int (&of)[3]) {
+    if (n <= 16) { of[0] = SHARED_FEW16; return 1; }
+    of[0] = SHARED_FEW32; of[1] = SHARED_FEW64; of[2] = SHARED_TILE;
+    return n <= 32 ? 1 : (n <= 64 ? 2 : 3);
+  };
+  int of_prefix[3] = {0}, of_tail[3] = {0};
+  const int n_of_prefix = c.prefix.n_seg > 0 ? bodies(rows, of_prefix) : 1, n_of_tail = c.tail.n_seg > 0 ? bodies(own_rows, of_tail) : 1;
+  PcSharedPlan best = {}, alone = {};
+  alone.alone = true;
+  const double one = own_rows <= 16 ? alone_us(c) : 1e30, launch = 6.0;  // (a second launch)
+  if (one < launch + 3.0) return alone;                      // (less than any cut)
+  double least = -1.0;
+  for (int i = 0; i < n_of_prefix; ++i)
+    for (int j = 0; j < n_of_tail; ++j) {
+      PcSharedPlan p = {};
+      if (c.prefix.n_seg > 0) p.prefix = side_of(c.n_prefix, rows, c.n_kv_heads, of_prefix[i] + (c.prefix.k_scale != nullptr));
+      if (c.tail.n_seg > 0) p.tail = side_of(c.batch, own_rows, c.n_kv_heads, of_tail[j] + (c.tail.k_scale != nullptr));
+      const double us = cut_of(c, p);
+      if (least < 0.0 || us < least) { least = us; best = p; }
+    }
+  if (one < least + launch) return alone;
+  best.prefix.runs = best.prefix.caches_heads * best.prefix.parts;
+  best.tail.runs = best.tail.caches_heads * best.tail.parts;
+  return best;
 }
 static long long workgroups(const PcSharedSide& s) { return s.body ? (s.runs * s.tiles + 7) / 8 * 8 : 0; }
 static int partials(const PcSharedPlan& p) { return p.prefix.parts + p.tail.parts; }
@@ -1072,18 +1110,16 @@ static int launch_rows(const PcSharedSide& s, const SharedArgs& a, const SharedA
     case SHARED_FEW32 + 1: return launch<D, SHARED_FEW32 + 1, OWN>(a, tail, n, n_tail, st);
     case SHARED_FEW64: return launch<D, SHARED_FEW64, OWN>(a, tail, n, n_tail, st);
     case SHARED_FEW64 + 1: return launch<D, SHARED_FEW64 + 1, OWN>(a, tail, n, n_tail, st);
-    case SHARED_FEW128: return launch<D, SHARED_FEW128, OWN>(a, tail, n, n_tail, st);
-    case SHARED_FEW128 + 1: return launch<D, SHARED_FEW128 + 1, OWN>(a, tail, n, n_tail, st);
     case SHARED_TILE: return launch<D, SHARED_TILE, OWN>(a, tail, n, n_tail, st);
     case SHARED_TILE + 1: return launch<D, SHARED_TILE + 1, OWN>(a, tail, n, n_tail, st);
     default: return PC_OK;                                   // no such rows
   }
 }
-template <int D, int PREFIX, int WAVES>
+template <int D, int PREFIX>
 static int launch_alone(const SharedArgs& p, const SharedArgs& t, long long n, hipStream_t st) {
-  const dim3 grid((unsigned)n), block(WAVES * PC_WAVE);
-  if (t.rows.k_scale) hipLaunchKernelGGL((shared_alone_kernel<D, PREFIX, true, WAVES>), grid, block, 0, st, p, t);
-  else hipLaunchKernelGGL((shared_alone_kernel<D, PREFIX, false, WAVES>), grid, block, 0, st, p, t);
+  const dim3 grid((unsigned)n), block(SHARED_ALONE * PC_WAVE);
+  if (t.rows.k_scale) hipLaunchKernelGGL((shared_alone_kernel<D, PREFIX, true>), grid, block, 0, st, p, t);
+  else hipLaunchKernelGGL((shared_alone_kernel<D, PREFIX, false>), grid, block, 0, st, p, t);
   PC_LAUNCH_CHECK();
   return PC_OK;
 }
@@ -1092,9 +1128,7 @@ static int launch_alone_of(const PcSharedCall& c, const SharedArgs& p, const Sha
   PcProfScope prof(PC_KERNEL_SHARED_TAIL, st);
   const long long n = (long long)c.batch * c.n_kv_heads;
   const int prefix = c.prefix.n_seg == 0 ? 0 : (c.prefix.k_scale ? 2 : 1);
-  if (n <= 512)
-    return prefix == 0 ? launch_alone<D, 0, 8>(p, t, n, st) : (prefix == 1 ? launch_alone<D, 1, 8>(p, t, n, st) : launch_alone<D, 2, 8>(p, t, n, st));
-  return prefix == 0 ? launch_alone<D, 0, 4>(p, t, n, st) : (prefix == 1 ? launch_alone<D, 1, 4>(p, t, n, st) : launch_alone<D, 2, 4>(p, t, n, st));
+  return prefix == 0 ? launch_alone<D, 0>(p, t, n, st) : (prefix == 1 ? launch_alone<D, 1>(p, t, n, st) : launch_alone<D, 2>(p, t, n, st));
 }
 
 template <int D>
