@@ -12,6 +12,9 @@
 //              transposed once on the way in, so that every wavefront reads them with 16 consecutive bytes a lane;
 //   tails      of up to 16 rows: one to eight wavefronts each, behind the prefix's workgroups in their launch.
 // Where few keys are shared, one launch takes every (sequence, KV head) for itself, prefix and tail (shared_alone).
+// Bound by memory up to some 170 rows (8-bit rows: 85), by the matrix cores and the softmax's vector instructions beyond.
+// Measured (8 KV heads of 128 values): 64 rows, 8 x 2048 keys, 16 tails of 512: 26 us (the loop at 28 GB/s a CU, then starts and
+// the merge); 64 rows, 32 x 2048 keys of 8 bits 49 us; 4096 rows, 8 x 2048 keys 343 us (0.81 PFLOP/s); 4 rows, 128 keys 7.4 us.
 // Rows of 8 bits: a code is a bf16 value exactly, the key's scale multiplies the logit in fp32, the value's scale the
 // probability in front of its rounding.  Rotated query rows keep two bf16 parts (2^-17), in row tiles one (2^-9: the
 // second would take LDS that the keys have).
@@ -1135,7 +1138,10 @@ template <int D>
 static int launch_merge(const SharedMergeArgs& m, hipStream_t st) {
   constexpr int GROUPS = 256 / (D / 4);
   PcProfScope prof(PC_KERNEL_SHARED_MERGE, st);
-  const bool wide = m.n_parts > 4 && m.n_rows * GROUPS < (1LL << 31);
+  // A workgroup's groups of threads share a row where rows are few and each group has more than one partial of it.  us a call, a
+  // row a group / a workgroup (128 values): 32 rows of 8 partials 23.6 / 23.5, of 25 16.8 / 13.8; 512 of 25 23.8 / 21.2;
+  // 2048 of 25 47.6 / 47.8; 8192 of 7 77.9 / 81.8; 512 of 16 and of 25 with 64 values 16.8 / 16.8, 17.6 / 15.5
+  const bool wide = m.n_parts > GROUPS && m.n_rows <= 1024;
   if (wide) hipLaunchKernelGGL((shared_merge_kernel<D, GROUPS>), dim3((unsigned)m.n_rows), dim3(256), 0, st, m);
   else hipLaunchKernelGGL((shared_merge_kernel<D, 1>), dim3((unsigned)((m.n_rows + GROUPS - 1) / GROUPS)), dim3(256), 0, st, m);
   PC_LAUNCH_CHECK();
