@@ -405,7 +405,7 @@ typedef struct pc_row_cache {
  *                                U { tail[b, g, j], j < visible } of q . k * scale, times the values
  * A key of a prefix is read from memory once for the query rows of all F sequences.
  *   q [B, n_q, H_q, D] bf16; q_pos [B] int32 (device), nullable: row t is rotated here at position
- *     pos0 + q_pos[b] + t >= 0 (rounded to bf16 once), so that the tails' lengths in front of the step serve
+ *     pos0 + q_pos[b] + t >= 0 (then kept to bf16 or better), so that the tails' lengths in front of the step serve
  *     as q_pos, with pos0 the position of a tail's first row; NULL: q arrives rotated.
  *   prefix: rows of n = n_prefix; NULL for none.   tail: rows of n = batch with n_seg = 1; NULL for none.
  *   tail_own: 0: every tail row is visible to every query row.  1: the tail's last n_q rows are the query rows'

@@ -330,6 +330,11 @@ class SharedPrefixDecoder:
         """q [B, n, H_q, D], k, v [B, n, H_kv, D] before RoPE, n <= max_rows: rows at positions tail_pos + len .. of
         their sequences.  Returns out [B, n, H_q, D] (a view of the step's buffer)."""
         n = q.shape[1]
+        if self.prefix_rows is None:
+            raise ValueError("load the documents first")
+        if not 1 <= n <= self.max_rows or q.shape != (self.B, n, self.Hq, self.D) or k.shape != (self.B, n, self.Hkv, self.D) or \
+                v.shape != k.shape:
+            raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}: not up to {self.max_rows} rows of this decoder")
         self._append(k, v, self.len)
         tail = B.make_row_cache(*self.tail, seg_len=self.len_new)
         if self.ws is None:
