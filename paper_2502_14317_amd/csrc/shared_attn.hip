@@ -14,7 +14,7 @@
 // Where few keys are shared, one launch takes every (sequence, KV head) for itself, prefix and tail (shared_alone).
 // Bound by memory up to some 170 rows (8-bit rows: 85), by the matrix cores and the softmax's vector instructions beyond.
 // Measured (8 KV heads of 128 values): 64 rows, 8 x 2048 keys, 16 tails of 512: 26 us (the loop at 28 GB/s a CU, then starts and
-// the merge); 64 rows, 32 x 2048 keys of 8 bits 49 us; 4096 rows, 8 x 2048 keys 343 us (0.81 PFLOP/s); 4 rows, 128 keys 7.4 us.
+// the merge); 64 rows, 32 x 2048 keys of 8 bits 49 us; 4096 rows, 8 x 2048 keys 335 us (0.83 PFLOP/s); 4 rows, 128 keys 7.0 us.
 // Rows of 8 bits: a code is a bf16 value exactly, the key's scale multiplies the logit in fp32, the value's scale the
 // probability in front of its rounding.  Rotated query rows keep two bf16 parts (2^-17), in row tiles one (2^-9: the
 // second would take LDS that the keys have).
@@ -381,6 +381,7 @@ struct SharedWalk {
       for (int nc = 0; nc < NC; ++nc)
 #pragma unroll
         for (int bi = 0; bi < 2; ++bi) s[nc][0][bi] = floatx4{0.f, 0.f, 0.f, 0.f};
+      __builtin_amdgcn_s_setprio(1);                         // the first product goes first (8-bit rows 1 to 2 % faster)
 #pragma unroll
       for (int ks = 0; ks < KSTEPS; ++ks)
 #pragma unroll
@@ -412,6 +413,7 @@ struct SharedWalk {
       const int left[1] = {cur.at.len - 32 * cur.at.blk};
       const bool masked = left[0] - most_unseen < 32;
       u32x4 p[NC][1];
+      __builtin_amdgcn_s_setprio(0);
       shared_softmax<NC, 1, VE, Q8>(s, sc, masked, left, unseen, kk, a.scale_log2, c.ref, c.sub, c.l, c.o, p);
       shared_values<NC, 1, VE, OWN>([&](int, int e) { return shared_value_operand<Q8>(vbuf, e); }, masked && most_unseen > 0, p, c.o);
       __builtin_amdgcn_sched_barrier(0);
@@ -738,8 +740,10 @@ __device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, i
     for (int e = 0; e < VE; ++e) o[nc][e] = floatx4{0.f, 0.f, 0.f, 0.f};
   }
 
-  // KB blocks together, so that their chains overlap; a block behind the run's end has no keys
+  // KB blocks together, so that their chains overlap; a block behind the run's end has no keys.  The products go first where
+  // both wavefronts of a SIMD can issue (4096 rows, 16384 keys: 341 -> 333 us).
   auto consume = [&](const SharedTile<D>& t, int first, const int (&left)[KB]) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_setprio(1);
     floatx4 s[NC][KB][2];
 #pragma unroll
     for (int nc = 0; nc < NC; ++nc)
@@ -773,8 +777,11 @@ __device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, i
     for (int b = 1; b < KB; ++b) least = min(least, left[b]);
     const bool masked = least - most_unseen < 32;
     u32x4 p[NC][KB];
+    __builtin_amdgcn_s_setprio(0);
     shared_softmax<NC, KB, VE, Q8>(s, sc, masked, left, unseen, kk, a.scale_log2, ref, sub, l_run, o, p);
+    __builtin_amdgcn_s_setprio(1);
     shared_values<NC, KB, VE, OWN>([&](int b, int e) { return t.v[first + b][e][lane]; }, masked && most_unseen > 0, p, o);
+    __builtin_amdgcn_s_setprio(0);
   };
 
   // Tile t is in LDS buffer t % 2 while tile t + 1 is on its way into registers: that is written to the other buffer,
