@@ -61,6 +61,20 @@ int pc_mfma_ceiling(int mode, int n_cus, int iters, float* scratch, size_t scrat
  * this machine.  PC_ERR_NULL / PC_ERR_SHAPE / PC_ERR_HIP. */
 int pc_copy_ceiling(int mode, const void* src, void* dst, size_t bytes, void* stream);
 
+/* ---- how a pc_shared_attn call is done (measurement aid; host only, launches nothing) ------------
+ * A side (prefix, tail): its format (0 no rows, 1 16-bit, 2 8-bit rows), the query rows a workgroup takes (16, 32, 64
+ * from memory straight into registers, 256 by tiles of keys in LDS; 0 no workgroups of its own) and the parts its keys
+ * are cut into.  alone: one launch for everything, both sides' workgroups with it.  tails_behind: the tails ride in the
+ * prefix's launch, tail_waves wavefronts a run of a tail's keys.  Sizes and formats as pc_shared_attn; PC_ERR_SHAPE. */
+typedef struct pc_shared_attn_plan_info {
+  int32_t alone;
+  int32_t prefix_format, prefix_rows, prefix_parts;
+  int32_t tail_format, tail_rows, tail_parts, tail_waves, tails_behind;
+} pc_shared_attn_plan_info;
+int pc_shared_attn_plan(const pc_row_cache* prefix, const pc_row_cache* tail, int32_t batch, int32_t n_prefix,
+                        int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                        pc_shared_attn_plan_info* plan);
+
 #ifdef __cplusplus
 }
 #endif

@@ -28,7 +28,7 @@ SYMBOLS = [
     "pc_copy_ceiling", "pc_decode_step", "pc_decode_step_workspace_bytes", "pc_decode_step_fp8",
     "pc_decode_step_fp8_workspace_bytes", "pc_layer_forward", "pc_layer_workspace_bytes",
     "pc_shared_attn", "pc_shared_attn_workspace_bytes", "pc_kv_append_row8", "pc_kv_read_row8",
-    "pc_verify_drafts", "pc_verify_drafts_workspace_bytes",
+    "pc_verify_drafts", "pc_verify_drafts_workspace_bytes", "pc_shared_attn_plan",
 ]
 
 
@@ -41,6 +41,11 @@ class pc_shape(Structure):
 class pc_row_cache(Structure):
     _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p), ("seg_len", c_void_p),
                 ("seg_len_per_head", c_int32), ("n_seg", c_int32), ("cap", c_int32)]
+
+
+class pc_shared_attn_plan_info(Structure):
+    _fields_ = [(name, c_int32) for name in ("alone", "prefix_format", "prefix_rows", "prefix_parts", "tail_format", "tail_rows",
+                                             "tail_parts", "tail_waves", "tails_behind")]
 
 
 class PcError(RuntimeError):
@@ -139,6 +144,8 @@ def lib():
     L.pc_shared_attn.restype = c_int
     L.pc_shared_attn_workspace_bytes.argtypes = [POINTER(pc_row_cache), POINTER(pc_row_cache)] + [c_int32] * 6
     L.pc_shared_attn_workspace_bytes.restype = c_size_t
+    L.pc_shared_attn_plan.argtypes = [POINTER(pc_row_cache), POINTER(pc_row_cache)] + [c_int32] * 6 + [POINTER(pc_shared_attn_plan_info)]
+    L.pc_shared_attn_plan.restype = c_int
     L.pc_kv_append_row8.argtypes = [P, P, P, c_int32, c_float] + [c_int32] * 5 + [P] * 7
     L.pc_kv_append_row8.restype = c_int
     L.pc_kv_read_row8.argtypes = [P] * 5 + [c_int32] * 4 + [P] * 3
@@ -413,6 +420,14 @@ def pc_shared_attn(q, prefix, tail, batch, n_prefix, n_q, n_q_heads, n_kv_heads,
     _check(lib().pc_shared_attn(_ptr(q), _ptr(q_pos), pos0, rope_base, softmax_scale, _rows_ref(prefix), _rows_ref(tail),
                                 int(bool(tail_own)), batch, n_prefix, n_q, n_q_heads, n_kv_heads, head_dim, _ptr(out),
                                 _ptr(lse_out), p, n, _stream()), "pc_shared_attn")
+
+
+def pc_shared_attn_plan(prefix, tail, batch, n_prefix, n_q, n_q_heads, n_kv_heads, head_dim):
+    """How a pc_shared_attn call of these sizes and formats is done, as a dict (launches nothing)."""
+    info = pc_shared_attn_plan_info()
+    _check(lib().pc_shared_attn_plan(_rows_ref(prefix), _rows_ref(tail), batch, n_prefix, n_q, n_q_heads, n_kv_heads, head_dim,
+                                     ctypes.byref(info)), "pc_shared_attn_plan")
+    return {name: getattr(info, name) for name, _ in info._fields_}
 
 
 def pc_kv_append_row8(k_new, v_new, batch, n_new, cap, n_kv_heads, head_dim, k8, v8, k_scale, v_scale, len_in, len_out,

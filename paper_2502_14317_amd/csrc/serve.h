@@ -53,6 +53,7 @@ struct PcSharedCall {
 struct PcSharedSide { int body, parts, waves; long long tiles, caches_heads, runs; };      // body 0: no such side; waves: of a run behind the prefix's
 struct PcSharedPlan { PcSharedSide prefix, tail; bool alone; };
 PcSharedPlan pc_shared_plan(const PcSharedCall& c);
+void pc_shared_plan_info(const PcSharedCall& c, const PcSharedPlan& p, pc_shared_attn_plan_info& info);
 bool pc_shared_fits(const PcSharedCall& c, const PcSharedPlan& p);
 size_t pc_shared_ws_bytes(const PcSharedCall& c, const PcSharedPlan& p);
 int pc_launch_shared_attn(const PcSharedCall& c, const PcSharedPlan& p, void* ws, hipStream_t st);

@@ -49,6 +49,18 @@ extern "C" size_t pc_shared_attn_workspace_bytes(const pc_row_cache* prefix, con
   return pc_shared_ws_bytes(c, plan);
 }
 
+extern "C" int pc_shared_attn_plan(const pc_row_cache* prefix, const pc_row_cache* tail, int32_t batch, int32_t n_prefix,
+                                   int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                                   pc_shared_attn_plan_info* plan_info) {
+  PcSharedCall c;
+  PcSharedPlan plan;
+  const int rc = check_shared_sizes(prefix, tail, batch, n_prefix, n_q, n_q_heads, n_kv_heads, head_dim, c, plan);
+  if (rc != PC_OK) return rc;
+  if (!plan_info) return PC_ERR_NULL;
+  pc_shared_plan_info(c, plan, *plan_info);
+  return PC_OK;
+}
+
 extern "C" int pc_shared_attn(const void* q, const int32_t* q_pos, int32_t pos0, float rope_base, float softmax_scale,
                               const pc_row_cache* prefix, const pc_row_cache* tail, int32_t tail_own, int32_t batch,
                               int32_t n_prefix, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,

@@ -1074,6 +1074,27 @@ PcSharedPlan pc_shared_plan(const PcSharedCall& c) {
 static long long workgroups(const PcSharedSide& s) { return s.body ? (s.runs * s.tiles + 7) / 8 * 8 : 0; }
 static int partials(const PcSharedPlan& p) { return p.prefix.parts + p.tail.parts; }
 
+// The one-launch kernel's bodies: 0 no keys, 1 16-bit, 2 8-bit rows (it has no body without a tail: an empty 16-bit one)
+struct AloneFormats { int prefix, tail; };
+static AloneFormats alone_formats(const PcSharedCall& c) {
+  return {c.prefix.n_seg == 0 ? 0 : (c.prefix.k_scale ? 2 : 1), c.tail.k_scale ? 2 : 1};
+}
+void pc_shared_plan_info(const PcSharedCall& c, const PcSharedPlan& p, pc_shared_attn_plan_info& info) {
+  info = {};
+  info.alone = p.alone;
+  if (p.alone) {
+    const auto f = alone_formats(c);
+    info.prefix_format = f.prefix; info.tail_format = f.tail;
+    info.prefix_rows = f.prefix ? 16 : 0; info.tail_rows = 16;
+    info.prefix_parts = f.prefix ? 1 : 0; info.tail_parts = 1; info.tail_waves = SHARED_ALONE;
+    return;
+  }
+  if (p.prefix.body) { info.prefix_format = 1 + p.prefix.body % 2; info.prefix_rows = shared_body_rows(p.prefix.body); info.prefix_parts = p.prefix.parts; }
+  if (p.tail.body) {
+    info.tail_format = 1 + p.tail.body % 2; info.tail_rows = shared_body_rows(p.tail.body); info.tail_parts = p.tail.parts;
+    info.tail_waves = p.tail.waves; info.tails_behind = tails_behind(p);
+  }
+}
 bool pc_shared_fits(const PcSharedCall& c, const PcSharedPlan& p) {
   return workgroups(p.prefix) + workgroups(p.tail) < (1LL << 32) / SHARED_THREADS &&
          (long long)c.batch * c.n_kv_heads < (1LL << 32) / SHARED_THREADS;
@@ -1126,9 +1147,9 @@ static int launch_rows(const PcSharedSide& s, const SharedArgs& a, const SharedA
   }
 }
 template <int D, int PREFIX>
-static int launch_alone(const SharedArgs& p, const SharedArgs& t, long long n, hipStream_t st) {
+static int launch_alone(const PcSharedCall& c, const SharedArgs& p, const SharedArgs& t, long long n, hipStream_t st) {
   const dim3 grid((unsigned)n), block(SHARED_ALONE * PC_WAVE);
-  if (t.rows.k_scale) hipLaunchKernelGGL((shared_alone_kernel<D, PREFIX, true>), grid, block, 0, st, p, t);
+  if (alone_formats(c).tail == 2) hipLaunchKernelGGL((shared_alone_kernel<D, PREFIX, true>), grid, block, 0, st, p, t);
   else hipLaunchKernelGGL((shared_alone_kernel<D, PREFIX, false>), grid, block, 0, st, p, t);
   PC_LAUNCH_CHECK();
   return PC_OK;
@@ -1137,8 +1158,8 @@ template <int D>
 static int launch_alone_of(const PcSharedCall& c, const SharedArgs& p, const SharedArgs& t, hipStream_t st) {
   PcProfScope prof(PC_KERNEL_SHARED_TAIL, st);
   const long long n = (long long)c.batch * c.n_kv_heads;
-  const int prefix = c.prefix.n_seg == 0 ? 0 : (c.prefix.k_scale ? 2 : 1);
-  return prefix == 0 ? launch_alone<D, 0>(p, t, n, st) : (prefix == 1 ? launch_alone<D, 1>(p, t, n, st) : launch_alone<D, 2>(p, t, n, st));
+  const int prefix = alone_formats(c).prefix;
+  return prefix == 0 ? launch_alone<D, 0>(c, p, t, n, st) : (prefix == 1 ? launch_alone<D, 1>(c, p, t, n, st) : launch_alone<D, 2>(c, p, t, n, st));
 }
 
 template <int D>
