@@ -408,6 +408,7 @@ typedef struct pc_row_cache {
  *     pos0 + q_pos[b] + t >= 0 (then kept to bf16 or better), so that the tails' lengths in front of the step serve
  *     as q_pos, with pos0 the position of a tail's first row; NULL: q arrives rotated.
  *   prefix: rows of n = n_prefix; NULL for none.   tail: rows of n = batch with n_seg = 1; NULL for none.
+ *     n_seg = 0 is none, too: its pointers are not looked at.
  *   tail_own: 0: every tail row is visible to every query row.  1: the tail's last n_q rows are the query rows'
  *     own: row t sees tail rows j < seg_len - (n_q - 1 - t) (append the rows first, then call).
  *   out [B, n_q, H_q, D] bf16; a row that sees no key is 0.   lse_out [B, H_q, n_q] fp32, nullable (natural log;

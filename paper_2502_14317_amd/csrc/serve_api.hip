@@ -28,6 +28,7 @@ static int check_shared_sizes(const pc_row_cache* prefix, const pc_row_cache* ta
     if (r->n_seg < 0 || r->n_seg > (i ? 1 : kMost) || r->cap < 1 || r->cap > (1 << 24)) return PC_ERR_SHAPE;
     if (r->seg_len_per_head != 0 && r->seg_len_per_head != 1) return PC_ERR_SHAPE;
     if ((long long)(i ? batch : n_prefix) * r->n_seg * n_kv_heads > 0x7fffffffLL / 64) return PC_ERR_SHAPE;
+    if (r->n_seg == 0) continue;         // nothing there: as if it were not given, its pointers are nobody's
     PcRows& to = i ? c.tail : c.prefix;
     to.k = r->k; to.v = r->v; to.k_scale = r->k_scale; to.v_scale = r->v_scale; to.len = r->seg_len;
     to.len_per_head = r->seg_len_per_head; to.n_seg = r->n_seg; to.cap = r->cap;
