@@ -25,7 +25,7 @@
 #define SHARED_THREADS (SHARED_WAVES * PC_WAVE)
 #define SHARED_LOG2E 1.4426950408889634f
 #define SHARED_LN2 0.6931471805599453f
-#define SHARED_WINDOW 8.0f   // log2 units a logit may exceed its row's reference before that moves
+#define SHARED_WINDOW 8.0f   // log2 units above a row's largest logit that its reference moves to, when a logit exceeds it
 
 struct SharedArgs {
   const uint16_t* q;
@@ -156,7 +156,9 @@ struct SharedQueryRows {
 };
 // KB blocks of 32 keys for NC blocks of columns: logits (lane: column c16, keys 16 bi + 4 kk + j of a block) ->
 // probabilities as the B operand of the second product, relative to the column's reference, which moves only when a
-// logit exceeds it by more than the window: then everything before is worth exp2(the move) of what it was.
+// logit exceeds it, and then to the window above that logit: everything before is worth exp2(the move) of what it was.  So a
+// probability is never above 1, and sums of values times probabilities stay inside fp32 wherever those relative to the row's
+// maximum do.
 // left[b]: keys of the block's segment from its first one on.
 struct SharedScales { floatx4 k[2], v[2]; };
 template <int NC, int KB, int VE, bool Q8>
@@ -195,13 +197,13 @@ __device__ __forceinline__ void shared_softmax(floatx4 (&s)[NC][KB][2], const Sh
 #pragma unroll
       for (int bi = 0; bi < 2; ++bi)
         top[nc] = fmaxf(fmaxf(top[nc], fmaxf(s[nc][b][bi][0], s[nc][b][bi][1])), fmaxf(s[nc][b][bi][2], s[nc][b][bi][3]));
-    beyond |= top[nc] * scale_log2 > ref[nc] + SHARED_WINDOW;
+    beyond |= top[nc] * scale_log2 > ref[nc];
   }
   if (__any(beyond)) {
 #pragma unroll
     for (int nc = 0; nc < NC; ++nc) {
       const float most = pc_rows_max(top[nc]) * scale_log2;
-      const float m = most > ref[nc] + SHARED_WINDOW ? most : ref[nc];      // (a column's results do not hang on the others')
+      const float m = most > ref[nc] ? most + SHARED_WINDOW : ref[nc];      // (a column's results do not hang on the others')
       sub[nc] = m == -INFINITY ? 0.f : m;                    // no key seen yet
       const float alpha = __builtin_amdgcn_exp2f(ref[nc] - sub[nc]);
       ref[nc] = m;
