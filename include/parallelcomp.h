@@ -410,7 +410,8 @@ typedef struct pc_row_cache {
  *   prefix: rows of n = n_prefix; NULL for none.   tail: rows of n = batch with n_seg = 1; NULL for none.
  *     n_seg = 0 is none, too: its pointers are not looked at.
  *   tail_own: 0: every tail row is visible to every query row.  1: the tail's last n_q rows are the query rows'
- *     own: row t sees tail rows j < seg_len - (n_q - 1 - t) (append the rows first, then call).
+ *     own: row t sees tail rows j < seg_len - (n_q - 1 - t) (append the rows first, then call).  All n_q have to be there:
+ *     where the append dropped some for want of room, the rows in front of them would be taken for them.
  *   out [B, n_q, H_q, D] bf16; a row that sees no key is 0.   lse_out [B, H_q, n_q] fp32, nullable (natural log;
  *     -inf where no key is seen).
  * Whatever lies in rows behind the lengths, and in rows that a query row does not see, stays out of its result,
@@ -436,7 +437,7 @@ size_t pc_shared_attn_workspace_bytes(const pc_row_cache* prefix, const pc_row_c
  *   k8, v8 [B, H_kv, cap, D] uint8, k_scale, v_scale [B, H_kv, cap] fp32 in/out
  *   len_in [B] int32 (device), nullable (all 0); len_out [B], nullable: min(len_in + n_new, cap).  They must not
  *   overlap: the rows of a sequence are written by many workgroups, each of which reads len_in.
- * batch * n_new * H_kv < 2^31.  Rows that do not fit are dropped.  A compacted cache [S, H_kv, k_t, D] of the gather is quantised by one call
+ * batch * n_new * H_kv < 2^31.  Rows that do not fit are dropped (len_out stays at cap).  A compacted cache [S, H_kv, k_t, D] of the gather is quantised by one call
  * with batch = S * H_kv, n_new = cap = k_t, one KV head.  No workspace. */
 int pc_kv_append_row8(const void* k_new, const void* v_new, const int32_t* pos, int32_t pos0, float rope_base, int32_t batch,
                       int32_t n_new, int32_t cap, int32_t n_kv_heads, int32_t head_dim, void* k8, void* v8,
@@ -461,7 +462,8 @@ int pc_kv_read_row8(const void* k8, const void* v8, const float* k_scale, const 
  * entry (the quotient correctly rounded): results do not depend on the order of the work.
  *   tokens [B, n_draft + 1] int32 out: the standing drafts, the next token, then -1;  n_accepted [B] int32 out
  *   len_in, len_out [B] int32 (device), both or neither: len_out = len_in + 1 + n_accepted, the rows of a cache
- *     that stand (the last token's and the standing drafts' behind len_in); may be the same array.
+ *     that stand (the last token's and the standing drafts' behind len_in), if all of them were written: no capacity is
+ *     known here, so the caller drafts no more rows than fit; may be the same array.
  * Workspace: pc_verify_drafts_workspace_bytes(batch, n_draft, vocab). */
 int pc_verify_drafts(const int32_t* draft, const int32_t* draft_len, const float* draft_prob,
                      const float* target_prob, const float* u, const float* noise, int32_t batch,

@@ -282,7 +282,9 @@ class SharedPrefixDecoder:
       step(q, k, v)   the n rows a sequence (its last token and the drafts behind it) of this layer
       accept()        all n rows stand (no drafts), or
       verify(...)     those up to the first draft that falls stand; the others' rows are written over by the next step.
-    Lengths live on the device, so a run of steps is a run of library calls with no host round trip."""
+    Lengths live on the device, so a run of steps is a run of library calls with no host round trip, until the rows written
+    so far could fill a tail: then a step reads the lengths, and raises if its rows would pass the capacity of one.  A step in
+    a captured graph cannot: whoever replays it sees to it that the rows fit."""
 
     def __init__(self, batch, n_prefix, n_seg, keep_tokens, tail_cap, n_q_heads, n_kv_heads, head_dim, rope_base,
                  tail_pos, max_rows=1, softmax_scale=0.0, eight_bit_prefix=False, device="cuda"):
@@ -301,6 +303,8 @@ class SharedPrefixDecoder:
         self.tail = rows8(batch, 1, n_kv_heads, tail_cap)
         self.len = torch.zeros((batch,), dtype=i32, device=device)          # rows of the tails that stand
         self.len_new = torch.zeros_like(self.len)                           # with those of the step at hand
+        self.rows = 0                                                       # rows of the step at hand
+        self.most = 0                                                       # no tail has more rows that stand; None: not known
         self.prefix_rows = None
         self.lse = torch.empty((batch, n_q_heads, max_rows), dtype=f32, device=device)
         self.out = torch.empty((batch, max_rows, n_q_heads, head_dim), dtype=torch.bfloat16, device=device)
@@ -309,6 +313,9 @@ class SharedPrefixDecoder:
     def load(self, kc, vc, seg_len=None, seg_len_per_head=0, k_tail=None, v_tail=None):
         """kc, vc [n_prefix, n_seg, H_kv, k_t, D] bf16 compacted segments (copied, or rounded to 8-bit rows), seg_len
         int32 or None (all k_t); k_tail, v_tail [B, n0, H_kv, D] rotated keys / values of the query blocks."""
+        n0 = 0 if k_tail is None else k_tail.shape[1]
+        if n0 > self.cap:
+            raise ValueError(f"the tails hold {self.cap} rows, not {n0}")
         if self.eight_bit_prefix:                                           # a segment's head is a sequence of its own
             k8, v8, ks, vs = self.prefix
             B.pc_kv_append_row8(kc, vc, self.P * self.S * self.Hkv, self.kt, self.kt, 1, self.D, k8, v8, ks, vs, None, None)
@@ -317,11 +324,27 @@ class SharedPrefixDecoder:
         self.prefix_rows = B.make_row_cache(*self.prefix, seg_len=seg_len, seg_len_per_head=seg_len_per_head)
         self.ws = None
         self.len.zero_()
+        self.rows = 0
+        if self.most is not None:
+            self.most = 0
         if k_tail is not None:
             self._append(k_tail, v_tail, None)
             self.accept()
 
+    def _room(self, n):
+        """Refuses n rows a sequence that would pass the capacity of a tail."""
+        if self.len.is_cuda and torch.cuda.is_current_stream_capturing():
+            self.most = None                                                # replays will move the lengths unseen
+            return
+        if self.most is None or self.most + n > self.cap:
+            most = int(self.len.max())
+            if self.most is not None:
+                self.most = most
+            if most + n > self.cap:
+                raise ValueError(f"the tails hold {self.cap} rows: {n} more do not fit behind the {most} of the longest")
+
     def _append(self, k, v, pos):
+        self.rows = k.shape[1]
         k8, v8, ks, vs = self.tail
         B.pc_kv_append_row8(k, v, self.B, k.shape[1], self.cap, self.Hkv, self.D, k8, v8, ks, vs, self.len, self.len_new,
                             pos=pos, pos0=self.pos0, rope_base=self.rope_base)
@@ -335,6 +358,7 @@ class SharedPrefixDecoder:
         if not 1 <= n <= self.max_rows or q.shape != (self.B, n, self.Hq, self.D) or k.shape != (self.B, n, self.Hkv, self.D) or \
                 v.shape != k.shape:
             raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}: not up to {self.max_rows} rows of this decoder")
+        self._room(n)
         self._append(k, v, self.len)
         tail = B.make_row_cache(*self.tail, seg_len=self.len_new)
         if self.ws is None:
@@ -350,8 +374,16 @@ class SharedPrefixDecoder:
     def accept(self):
         """Every row of the step stands."""
         self.len, self.len_new = self.len_new, self.len
+        self._stand(self.rows)
+
+    def _stand(self, n):
+        """The step at hand is done: up to n of its rows stand."""
+        self.rows = 0
+        if self.most is not None:
+            self.most += n
 
     def verify(self, draft, draft_prob, target_prob, u, noise, tokens, n_accepted, ws, draft_len=None):
         """pc_verify_drafts; the rows of the last token and of the standing drafts stay in the tails."""
         B.pc_verify_drafts(draft, draft_prob, target_prob, u, noise, self.B, draft.shape[1], target_prob.shape[2], tokens,
                            n_accepted, ws, draft_len=draft_len, len_in=self.len, len_out=self.len)
+        self._stand(draft.shape[1] + 1)

@@ -1,0 +1,112 @@
+"""SharedPrefixDecoder on the CPU, over a stand-in for the library that keeps the lengths as the calls do: what it refuses,
+before anything is written, and which rows it counts."""
+import pytest
+import torch
+
+from paper_2502_14317_amd import layer
+
+B, P, S, KT, CAP, HQ, HKV, D, V = 4, 2, 3, 16, 12, 8, 2, 64, 50
+
+
+class Library:
+    """Lengths as pc_kv_append_row8 and pc_verify_drafts leave them; `accepted` says how many drafts stand."""
+
+    def __init__(self):
+        self.calls, self.accepted = [], None
+
+    def make_row_cache(self, *tensors, **lens):
+        return object()
+
+    def alloc_workspace(self, n, device):
+        return None
+
+    def pc_shared_attn_workspace_bytes(self, *sizes):
+        return 256
+
+    def pc_kv_append_row8(self, k, v, batch, n, cap, hkv, d, k8, v8, ks, vs, len_in, len_out, **rotation):
+        self.calls.append(("append", n))
+        if len_out is not None:
+            assert len_out.data_ptr() != len_in.data_ptr()
+            len_out.copy_((len_in.clamp(0, cap) + n).clamp(max=cap))
+
+    def pc_shared_attn(self, q, *args, **kw):
+        self.calls.append(("attention", q.shape[1]))
+
+    def pc_verify_drafts(self, draft, *args, len_in, len_out, **kw):
+        self.calls.append(("verify", draft.shape[1]))
+        len_out.copy_(len_in + 1 + torch.tensor(self.accepted, dtype=torch.int32))
+
+
+def bf(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+def rows(n):
+    return bf(B, n, HQ, D), bf(B, n, HKV, D), bf(B, n, HKV, D)
+
+
+def drafts(k):
+    i32 = lambda *shape: torch.zeros(shape, dtype=torch.int32)
+    return dict(draft=i32(B, k), draft_prob=torch.zeros(B, k, V), target_prob=torch.zeros(B, k + 1, V), u=torch.zeros(B, k),
+                noise=torch.ones(B, V), tokens=i32(B, k + 1), n_accepted=i32(B), ws=None)
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    lib = Library()
+    monkeypatch.setattr(layer, "B", lib)
+    return lib
+
+
+def decoder(n0=0, eight_bit_prefix=False, max_rows=4):
+    d = layer.SharedPrefixDecoder(B, P, S, KT, CAP, HQ, HKV, D, 1e4, 100, max_rows=max_rows, eight_bit_prefix=eight_bit_prefix, device="cpu")
+    kc = bf(P, S, HKV, KT, D)
+    d.load(kc, kc, k_tail=bf(B, n0, HKV, D) if n0 else None, v_tail=bf(B, n0, HKV, D) if n0 else None)
+    return d
+
+
+def test_a_step_that_would_pass_the_capacity(lib):
+    d = decoder(CAP - 2)
+    lib.calls.clear()
+    before, new = d.len.clone(), d.len_new.clone()
+    for n in (3, 4):
+        with pytest.raises(ValueError, match="hold 12 rows"):
+            d.step(*rows(n))
+    assert lib.calls == [] and torch.equal(d.len, before) and torch.equal(d.len_new, new)
+    d.step(*rows(2))                                                        # these fit
+    d.accept()
+    assert d.len.tolist() == [CAP] * B
+    with pytest.raises(ValueError, match="hold 12 rows"):
+        d.step(*rows(1))
+
+
+def test_drafts_that_fell_leave_room(lib):
+    """The rows of fallen drafts are written over: the count of rows that may stand is settled by the lengths themselves."""
+    d = decoder()
+    for step in range(4):                                                   # 4 x 4 rows were written, 3 sequences keep 2 of each 4
+        d.step(*rows(4))
+        lib.accepted = [1, 1, 0, 1]
+        d.verify(**drafts(3))
+    assert d.len.tolist() == [8, 8, 4, 8]
+    d.step(*rows(4))
+    lib.accepted = [3, 0, 0, 0]
+    d.verify(**drafts(3))
+    assert d.len.tolist() == [CAP, 9, 5, 9]
+    with pytest.raises(ValueError, match="hold 12 rows"):                   # one sequence is full
+        d.step(*rows(1))
+
+
+def test_a_query_block_longer_than_the_tails(lib):
+    with pytest.raises(ValueError, match="hold 12 rows"):
+        decoder(CAP + 1)
+    assert lib.calls == []
+    assert decoder(CAP).len.tolist() == [CAP] * B
+
+
+def test_a_second_load_starts_anew(lib):
+    d = decoder(CAP)
+    kc = bf(P, S, HKV, KT, D)
+    d.load(kc, kc)
+    d.step(*rows(4))
+    d.accept()
+    assert d.len.tolist() == [4] * B
