@@ -284,7 +284,8 @@ class SharedPrefixDecoder:
       verify(...)     those up to the first draft that falls stand; the others' rows are written over by the next step.
     Lengths live on the device, so a run of steps is a run of library calls with no host round trip, until the rows written
     so far could fill a tail: then a step reads the lengths, and raises if its rows would pass the capacity of one.  A step in
-    a captured graph cannot: whoever replays it sees to it that the rows fit."""
+    a captured graph cannot: whoever replays it sees to it that the rows fit.  A graph of step and accept or verify goes on
+    from replay to replay; it is captured anew where load was given other lengths of the segments."""
 
     def __init__(self, batch, n_prefix, n_seg, keep_tokens, tail_cap, n_q_heads, n_kv_heads, head_dim, rope_base,
                  tail_pos, max_rows=1, softmax_scale=0.0, eight_bit_prefix=False, device="cuda"):
@@ -322,7 +323,6 @@ class SharedPrefixDecoder:
         else:
             self.prefix[0].copy_(kc); self.prefix[1].copy_(vc)
         self.prefix_rows = B.make_row_cache(*self.prefix, seg_len=seg_len, seg_len_per_head=seg_len_per_head)
-        self.ws = None
         self.len.zero_()
         self.rows = 0
         if self.most is not None:
@@ -373,7 +373,8 @@ class SharedPrefixDecoder:
 
     def accept(self):
         """Every row of the step stands."""
-        self.len, self.len_new = self.len_new, self.len
+        # no rows more, the lengths alone: in place, since a captured step reads them where they were when it was captured
+        B.pc_kv_append_row8(None, None, self.B, 0, self.cap, self.Hkv, self.D, None, None, None, None, self.len_new, self.len)
         self._stand(self.rows)
 
     def _stand(self, n):

@@ -18,7 +18,7 @@ class Library:
         return object()
 
     def alloc_workspace(self, n, device):
-        return None
+        return object()
 
     def pc_shared_attn_workspace_bytes(self, *sizes):
         return 256
@@ -110,3 +110,18 @@ def test_a_second_load_starts_anew(lib):
     d.step(*rows(4))
     d.accept()
     assert d.len.tolist() == [4] * B
+
+
+def test_lengths_and_workspace_stay_where_they_are(lib):
+    """What a captured step has taken in: the same lengths are read and written by every step."""
+    d = decoder(2)
+    at = d.len.data_ptr(), d.len_new.data_ptr()
+    for _ in range(2):
+        d.step(*rows(1))
+        d.accept()
+        assert (d.len.data_ptr(), d.len_new.data_ptr()) == at
+    assert d.len.tolist() == [4] * B
+    ws = d.ws
+    d.load(*[bf(P, S, HKV, KT, D)] * 2)
+    d.step(*rows(1))
+    assert d.ws is ws is not None
