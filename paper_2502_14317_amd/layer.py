@@ -272,6 +272,11 @@ class DecodeCacheFp8:
         return self.out
 
 
+def _capturing(t):
+    """Is work on t's device being recorded into a graph here?"""
+    return t.is_cuda and torch.cuda.is_current_stream_capturing()
+
+
 class SharedPrefixDecoder:
     """Many answers over few compressed documents: n_prefix documents' compacted segments, each shared by batch /
     n_prefix sequences (sequence b reads document b // (batch // n_prefix)), and a tail a sequence that starts as its
@@ -304,7 +309,8 @@ class SharedPrefixDecoder:
         self.tail = rows8(batch, 1, n_kv_heads, tail_cap)
         self.len = torch.zeros((batch,), dtype=i32, device=device)          # rows of the tails that stand
         self.len_new = torch.zeros_like(self.len)                           # with those of the step at hand
-        self.rows = 0                                                       # rows of the step at hand
+        self.rows = 0                                                       # rows of the step at hand; 0: none
+        self.graph_rows = 0                                                 # of the longest step that a graph holds
         self.most = 0                                                       # no tail has more rows that stand; None: not known
         self.prefix_rows = None
         self.lse = torch.empty((batch, n_q_heads, max_rows), dtype=f32, device=device)
@@ -327,14 +333,15 @@ class SharedPrefixDecoder:
         self.rows = 0
         if self.most is not None:
             self.most = 0
-        if k_tail is not None:
+        if n0 > 0:
             self._append(k_tail, v_tail, None)
             self.accept()
 
     def _room(self, n):
         """Refuses n rows a sequence that would pass the capacity of a tail."""
-        if self.len.is_cuda and torch.cuda.is_current_stream_capturing():
+        if _capturing(self.len):
             self.most = None                                                # replays will move the lengths unseen
+            self.graph_rows = max(self.graph_rows, n)
             return
         if self.most is None or self.most + n > self.cap:
             most = int(self.len.max())
@@ -344,10 +351,10 @@ class SharedPrefixDecoder:
                 raise ValueError(f"the tails hold {self.cap} rows: {n} more do not fit behind the {most} of the longest")
 
     def _append(self, k, v, pos):
-        self.rows = k.shape[1]
         k8, v8, ks, vs = self.tail
         B.pc_kv_append_row8(k, v, self.B, k.shape[1], self.cap, self.Hkv, self.D, k8, v8, ks, vs, self.len, self.len_new,
                             pos=pos, pos0=self.pos0, rope_base=self.rope_base)
+        self.rows = k.shape[1]
 
     def step(self, q, k, v):
         """q [B, n, H_q, D], k, v [B, n, H_kv, D] before RoPE, n <= max_rows: rows at positions tail_pos + len .. of
@@ -373,9 +380,16 @@ class SharedPrefixDecoder:
 
     def accept(self):
         """Every row of the step stands."""
+        self._written(1)
         # no rows more, the lengths alone: in place, since a captured step reads them where they were when it was captured
         B.pc_kv_append_row8(None, None, self.B, 0, self.cap, self.Hkv, self.D, None, None, None, None, self.len_new, self.len)
         self._stand(self.rows)
+
+    def _written(self, n):
+        """Refuses to count n rows a sequence that the step at hand, or a graph's where there is none, has not written."""
+        rows = self.rows or self.graph_rows
+        if n > rows:
+            raise ValueError(f"{n} rows a sequence to stand, {rows} rows of the step at hand")
 
     def _stand(self, n):
         """The step at hand is done: up to n of its rows stand."""
@@ -384,7 +398,9 @@ class SharedPrefixDecoder:
             self.most += n
 
     def verify(self, draft, draft_prob, target_prob, u, noise, tokens, n_accepted, ws, draft_len=None):
-        """pc_verify_drafts; the rows of the last token and of the standing drafts stay in the tails."""
+        """pc_verify_drafts; the rows of the last token and of the standing drafts stay in the tails.  No more drafts than
+        rows behind the first that the step has written."""
+        self._written(draft.shape[1] + 1)
         B.pc_verify_drafts(draft, draft_prob, target_prob, u, noise, self.B, draft.shape[1], target_prob.shape[2], tokens,
                            n_accepted, ws, draft_len=draft_len, len_in=self.len, len_out=self.len)
         self._stand(draft.shape[1] + 1)

@@ -125,3 +125,44 @@ def test_lengths_and_workspace_stay_where_they_are(lib):
     d.load(*[bf(P, S, HKV, KT, D)] * 2)
     d.step(*rows(1))
     assert d.ws is ws is not None
+
+
+def test_verification_of_rows_that_were_not_written(lib):
+    d = decoder(2)
+    with pytest.raises(ValueError, match="rows of the step"):               # no step at all
+        d.verify(**drafts(0))
+    with pytest.raises(ValueError, match="rows of the step"):
+        d.accept()
+    d.step(*rows(2))
+    lib.calls.clear()
+    with pytest.raises(ValueError, match="rows of the step"):
+        d.verify(**drafts(2))
+    assert lib.calls == [] and d.len.tolist() == [2] * B
+    lib.accepted = [1, 0, 1, 0]
+    d.verify(**drafts(1))
+    assert d.len.tolist() == [4, 3, 4, 3]
+    with pytest.raises(ValueError, match="rows of the step"):               # once only
+        d.verify(**drafts(1))
+    d.step(*rows(3))                                                        # fewer drafts than rows are fine
+    lib.accepted = [0] * 4
+    d.verify(**drafts(0))
+    assert d.len.tolist() == [5, 4, 5, 4]
+
+
+def test_steps_in_a_graph_may_be_verified_outside(lib, monkeypatch):
+    """Who replays a captured step verifies its rows after every replay."""
+    d = decoder(2)
+    monkeypatch.setattr(layer, "_capturing", lambda t: True)
+    d.step(*rows(3))
+    monkeypatch.setattr(layer, "_capturing", lambda t: False)
+    lib.accepted = [0] * 4
+    for _ in range(3):
+        d.verify(**drafts(2))
+    with pytest.raises(ValueError, match="rows of the step"):
+        d.verify(**drafts(3))
+    assert d.len.tolist() == [5] * B
+    d.step(*rows(1))                                                        # an eager step counts for itself
+    with pytest.raises(ValueError, match="rows of the step"):
+        d.verify(**drafts(2))
+    d.accept()
+    assert d.len.tolist() == [6] * B
