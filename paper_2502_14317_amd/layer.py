@@ -277,6 +277,14 @@ def _capturing(t):
     return t.is_cuda and torch.cuda.is_current_stream_capturing()
 
 
+def _must_be(shape, dtype, **tensors):
+    """Refuses tensors whose memory is not a whole [shape] of dtype: the library is given addresses."""
+    for name, t in tensors.items():
+        if t is None or t.shape != shape or t.dtype != dtype or not t.is_contiguous():
+            got = t if t is None else f"{t.dtype} {tuple(t.shape)}, strides {t.stride()}"
+            raise ValueError(f"{name}: {got} is not {dtype} {tuple(shape)}, contiguous")
+
+
 class SharedPrefixDecoder:
     """Many answers over few compressed documents: n_prefix documents' compacted segments, each shared by batch /
     n_prefix sequences (sequence b reads document b // (batch // n_prefix)), and a tail a sequence that starts as its
@@ -315,20 +323,29 @@ class SharedPrefixDecoder:
         self.prefix_rows = None
         self.lse = torch.empty((batch, n_q_heads, max_rows), dtype=f32, device=device)
         self.out = torch.empty((batch, max_rows, n_q_heads, head_dim), dtype=torch.bfloat16, device=device)
-        self.ws = None
+        self.ws = self.tail_rows = None                                     # made with the first step
 
     def load(self, kc, vc, seg_len=None, seg_len_per_head=0, k_tail=None, v_tail=None):
         """kc, vc [n_prefix, n_seg, H_kv, k_t, D] bf16 compacted segments (copied, or rounded to 8-bit rows), seg_len
-        int32 or None (all k_t); k_tail, v_tail [B, n0, H_kv, D] rotated keys / values of the query blocks."""
-        n0 = 0 if k_tail is None else k_tail.shape[1]
+        int32 or None (all k_t); k_tail, v_tail [B, n0, H_kv, D] bf16 rotated keys / values of the query blocks, or None."""
+        seg = (self.P, self.S, self.Hkv, self.kt, self.D)
+        if self.eight_bit_prefix:
+            _must_be(seg, torch.bfloat16, kc=kc, vc=vc)
+        elif kc.shape != seg or vc.shape != seg:
+            raise ValueError(f"kc {tuple(kc.shape)}, vc {tuple(vc.shape)}: not {seg}")
+        n0 = 0
+        if k_tail is not None or v_tail is not None:
+            n0 = 0 if k_tail is None or k_tail.dim() != 4 else k_tail.shape[1]
+            _must_be((self.B, n0, self.Hkv, self.D), torch.bfloat16, k_tail=k_tail, v_tail=v_tail)
         if n0 > self.cap:
             raise ValueError(f"the tails hold {self.cap} rows, not {n0}")
+        prefix_rows = B.make_row_cache(*self.prefix, seg_len=seg_len, seg_len_per_head=seg_len_per_head)
         if self.eight_bit_prefix:                                           # a segment's head is a sequence of its own
             k8, v8, ks, vs = self.prefix
             B.pc_kv_append_row8(kc, vc, self.P * self.S * self.Hkv, self.kt, self.kt, 1, self.D, k8, v8, ks, vs, None, None)
         else:
             self.prefix[0].copy_(kc); self.prefix[1].copy_(vc)
-        self.prefix_rows = B.make_row_cache(*self.prefix, seg_len=seg_len, seg_len_per_head=seg_len_per_head)
+        self.prefix_rows = prefix_rows
         self.len.zero_()
         self.rows = 0
         if self.most is not None:
@@ -357,7 +374,7 @@ class SharedPrefixDecoder:
         self.rows = k.shape[1]
 
     def step(self, q, k, v):
-        """q [B, n, H_q, D], k, v [B, n, H_kv, D] before RoPE, n <= max_rows: rows at positions tail_pos + len .. of
+        """q [B, n, H_q, D], k, v [B, n, H_kv, D] bf16 before RoPE, n <= max_rows: rows at positions tail_pos + len .. of
         their sequences.  Returns out [B, n, H_q, D] (a view of the step's buffer)."""
         n = q.shape[1]
         if self.prefix_rows is None:
@@ -365,10 +382,14 @@ class SharedPrefixDecoder:
         if not 1 <= n <= self.max_rows or q.shape != (self.B, n, self.Hq, self.D) or k.shape != (self.B, n, self.Hkv, self.D) or \
                 v.shape != k.shape:
             raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}: not up to {self.max_rows} rows of this decoder")
+        for t in (q, k, v):
+            if t.dtype != torch.bfloat16 or not t.is_contiguous():
+                raise ValueError("q, k and v must be bfloat16 and contiguous")
         self._room(n)
         self._append(k, v, self.len)
-        tail = B.make_row_cache(*self.tail, seg_len=self.len_new)
-        if self.ws is None:
+        tail = self.tail_rows
+        if tail is None:
+            tail = self.tail_rows = B.make_row_cache(*self.tail, seg_len=self.len_new)
             self.ws = B.alloc_workspace(max(B.pc_shared_attn_workspace_bytes(self.prefix_rows, tail, self.B, self.P, m, self.Hq,
                                                                              self.Hkv, self.D)
                                             for m in range(1, self.max_rows + 1)), q.device)
@@ -400,7 +421,18 @@ class SharedPrefixDecoder:
     def verify(self, draft, draft_prob, target_prob, u, noise, tokens, n_accepted, ws, draft_len=None):
         """pc_verify_drafts; the rows of the last token and of the standing drafts stay in the tails.  No more drafts than
         rows behind the first that the step has written."""
-        self._written(draft.shape[1] + 1)
-        B.pc_verify_drafts(draft, draft_prob, target_prob, u, noise, self.B, draft.shape[1], target_prob.shape[2], tokens,
-                           n_accepted, ws, draft_len=draft_len, len_in=self.len, len_out=self.len)
-        self._stand(draft.shape[1] + 1)
+        k, V, i32, f32 = draft.shape[1], target_prob.shape[-1], torch.int32, torch.float32
+        self._written(k + 1)
+        _must_be((self.B, k), i32, draft=draft)
+        _must_be((self.B, k), f32, u=u)
+        _must_be((self.B, k + 1, V), f32, target_prob=target_prob)
+        _must_be((self.B, V), f32, noise=noise)
+        _must_be((self.B, k + 1), i32, tokens=tokens)
+        _must_be((self.B,), i32, n_accepted=n_accepted)
+        if draft_prob is not None:
+            _must_be((self.B, k, V), f32, draft_prob=draft_prob)
+        if draft_len is not None:
+            _must_be((self.B,), i32, draft_len=draft_len)
+        B.pc_verify_drafts(draft, draft_prob, target_prob, u, noise, self.B, k, V, tokens, n_accepted, ws,
+                           draft_len=draft_len, len_in=self.len, len_out=self.len)
+        self._stand(k + 1)

@@ -166,3 +166,65 @@ def test_steps_in_a_graph_may_be_verified_outside(lib, monkeypatch):
         d.verify(**drafts(2))
     d.accept()
     assert d.len.tolist() == [6] * B
+
+
+def changed(args, **change):
+    return {**args, **change}
+
+
+@pytest.mark.parametrize("eight_bit", [False, True], ids=["16bit", "8bit"])
+def test_documents_of_another_shape_or_type(lib, eight_bit):
+    """In 8 bits the segments' addresses go to the library: nothing but its own shape and type does.  16-bit ones are copied,
+    which converts types."""
+    d = decoder(2, eight_bit)
+    d.step(*rows(1))
+    lib.calls.clear()
+    good, tail = bf(P, S, HKV, KT, D), bf(B, 2, HKV, D)
+    held = [x.clone() for x in (*d.prefix, d.len, d.len_new)]
+    one = good + 1
+    bad = [dict(kc=one[:, :1]), dict(vc=one[:, :, :, :KT - 1]), dict(kc=one[:1]), dict(vc=one.view(P, S, HKV, D, KT)), dict(kc=one[None])]
+    if eight_bit:
+        bad += [dict(kc=one.float()), dict(vc=one.half())]
+    bad += [dict(k_tail=tail[:, :1]), dict(v_tail=tail[:1]), dict(k_tail=tail.float()), dict(v_tail=tail.half()), dict(v_tail=None),
+            dict(k_tail=None), dict(k_tail=tail[0]), dict(k_tail=bf(B, 2, HQ, D), v_tail=bf(B, 2, HQ, D))]
+    for change in bad:
+        with pytest.raises(ValueError):
+            d.load(**changed(dict(kc=one, vc=one, k_tail=tail, v_tail=tail), **change))
+        assert lib.calls == [] and all(torch.equal(x, y) for x, y in zip(held, (*d.prefix, d.len, d.len_new))), change
+    d.accept()                                                              # the step at hand is still there
+    assert d.len.tolist() == [3] * B
+    d.load(good, good, k_tail=tail, v_tail=tail)
+    if not eight_bit:
+        d.load(one.float(), one.half(), k_tail=tail, v_tail=tail)
+        assert torch.equal(d.prefix[0], one) and torch.equal(d.prefix[1], one)
+
+
+def test_rows_of_another_type(lib):
+    d = decoder(2)
+    lib.calls.clear()
+    for at in range(3):
+        for dtype in (torch.float32, torch.float16):
+            args = [x.to(dtype) if i == at else x for i, x in enumerate(rows(2))]
+            with pytest.raises(ValueError, match="bfloat16"):
+                d.step(*args)
+    assert lib.calls == [] and d.len_new.tolist() == [2] * B
+
+
+def test_verification_of_another_shape_or_type(lib):
+    d = decoder(2)
+    d.step(*rows(4))
+    lib.calls.clear()
+    lib.accepted = [1] * 4
+    good = drafts(3)
+    bad = [dict(draft=good["draft"].long()), dict(draft=good["draft"][:2]), dict(draft_prob=good["draft_prob"][:, :2]),
+           dict(draft_prob=good["draft_prob"].half()), dict(target_prob=good["target_prob"][:, :3]), dict(target_prob=good["target_prob"].double()),
+           dict(draft_prob=good["draft_prob"][:, :, :V - 1]), dict(u=good["u"][:, :2]), dict(u=good["u"].half()), dict(noise=good["noise"][:2]),
+           dict(noise=good["noise"].half()), dict(noise=good["noise"][:, :V - 1]), dict(tokens=good["tokens"][:, :3]), dict(tokens=good["tokens"].long()),
+           dict(n_accepted=good["n_accepted"][:3]), dict(n_accepted=good["n_accepted"].long()),
+           dict(draft_len=torch.zeros(B)), dict(draft_len=torch.zeros(B - 1, dtype=torch.int32))]
+    for change in bad:
+        with pytest.raises(ValueError):
+            d.verify(**changed(good, **change))
+        assert lib.calls == [] and d.len.tolist() == [2] * B, change
+    d.verify(**changed(good, draft_prob=None, draft_len=torch.zeros(B, dtype=torch.int32)))
+    assert d.len.tolist() == [4] * B
