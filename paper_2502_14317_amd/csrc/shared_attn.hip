@@ -631,21 +631,22 @@ struct SharedTile {
   u32x4 v[SHARED_BLOCKS][D / 16][PC_WAVE];          // [block][operand e of V^T]
   float scale[2][SHARED_BLOCKS][32];                // [keys, values][block]
 };
-template <int D, int NC>
+#define SHARED_TILE_ROWS (SHARED_WAVES * 32)
+template <int D>
 struct SharedTilesLds {
   union {
     SharedTile<D> tile[2];
-    uint16_t q[SHARED_WAVES * 16 * NC][D + 8];
+    uint16_t q[SHARED_TILE_ROWS][D + 8];
   };
 };
 
-template <int D, int NC, bool Q8, bool OWN>
-__device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, int tile, SharedTilesLds<D, NC>& sm) {
-  constexpr int KSTEPS = D / 32, VE = D / 16, ELEM = Q8 ? 1 : 2, ROW = D * ELEM, KB = NC == 2 ? 2 : 1;
+template <int D, bool Q8, bool OWN>
+__device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, int tile, SharedTilesLds<D>& sm) {
+  constexpr int KSTEPS = D / 32, VE = D / 16, ELEM = Q8 ? 1 : 2, ROW = D * ELEM, NC = 2, KB = 2;
   typedef uint32_t piece_t __attribute__((ext_vector_type(VE * ELEM / 4)));
   const int lane = threadIdx.x % PC_WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PC_WAVE);
   const int kk = lane / 16, c16 = lane % 16;
-  const SharedPlace x = shared_place(a, run, tile, SHARED_WAVES * 16 * NC);
+  const SharedPlace x = shared_place(a, run, tile, SHARED_TILE_ROWS);
   const PcSegLens lens = shared_lens(a, x);
   auto next = [&](const SharedBlock& b) { return shared_block(a, x, pc_blocks_next(lens, b.at)); };
 
@@ -716,8 +717,7 @@ __device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, i
 
   // ---- the query rows; meanwhile the first tile is on its way
   const int first_lens = pc_first_lens(lens, lane);
-  constexpr int ROWS = SHARED_WAVES * 16 * NC;
-  SharedQueryRows<D, ROWS, SHARED_WAVES> rows;
+  SharedQueryRows<D, SHARED_TILE_ROWS, SHARED_WAVES> rows;
   rows.begin(a, x, threadIdx.x);
   SharedBlock last = shared_block(a, x, pc_blocks_begin<1>(lens, x.part, a.n_parts, a.parts_div, 0, lane, first_lens));
   Left at = issue(pieces, last);                            // the tile at hand
@@ -793,15 +793,8 @@ __device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, i
   Left ahead = issue(pieces, last);                         // the one on its way
   PC_LDS_BARRIER();
   for (int buf = 0; at.b0 > 0; buf ^= 1) {
-    if constexpr (KB == 2) {
-      consume(sm.tile[buf], 0, {at.b0, at.b1});
-      if (at.b2 > 0) consume(sm.tile[buf], 2, {at.b2, at.b3});
-    } else {
-      consume(sm.tile[buf], 0, {at.b0});
-      if (at.b1 > 0) consume(sm.tile[buf], 1, {at.b1});
-      if (at.b2 > 0) consume(sm.tile[buf], 2, {at.b2});
-      if (at.b3 > 0) consume(sm.tile[buf], 3, {at.b3});
-    }
+    consume(sm.tile[buf], 0, {at.b0, at.b1});
+    if (at.b2 > 0) consume(sm.tile[buf], 2, {at.b2, at.b3});
     commit(buf ^ 1, pieces);
     at = ahead;
     last = next(last);
@@ -914,13 +907,13 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedMergeArgs a) {
 // ------------------------------------------------------------------------------------------ launches
 // What a launch's workgroups are: few rows (16, 32 or 64 of them), row tiles of 256 rows; odd numbers: 8-bit rows
 enum SharedBody { SHARED_FEW16 = 2, SHARED_FEW32 = 4, SHARED_FEW64 = 6, SHARED_TILE = 8 };
-static constexpr int shared_body_rows(int body) { return body >= SHARED_TILE ? 256 : 8 << body / 2; }
+static constexpr int shared_body_rows(int body) { return body >= SHARED_TILE ? SHARED_TILE_ROWS : 8 << body / 2; }
 template <int D, int BODY>
 struct SharedBodyOf {
   static constexpr bool Q8 = BODY % 2, FEW = BODY < SHARED_TILE;
-  static constexpr int ROWS = shared_body_rows(BODY), NC = FEW ? (ROWS < 32 ? 1 : 2) : ROWS / (16 * SHARED_WAVES), WR = FEW ? ROWS / (16 * NC) : 1;
+  static constexpr int ROWS = shared_body_rows(BODY), NC = ROWS < 32 ? 1 : 2, WR = FEW ? ROWS / (16 * NC) : 1;
   typedef SharedFewLds<D, NC, WR, SHARED_WAVES> FewLds;
-  static constexpr int LDS = FEW ? sizeof(FewLds) : sizeof(SharedTilesLds<D, NC>);
+  static constexpr int LDS = FEW ? sizeof(FewLds) : sizeof(SharedTilesLds<D>);
 };
 // Partials of `a`'s keys: OWN, of tails; else of prefixes, and behind their n_first workgroups those of the tails of up
 // to 16 rows.  An XCD (number mod 8) has an eighth of (run, tile), the tiles of a run behind each other: its L2 serves
@@ -938,7 +931,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_rows_kernel(SharedAr
   if (at >= a.n_runs * a.n_tiles) return;
   const int run = pc_div(at, a.tiles_div), tile = at - run * a.n_tiles;
   if constexpr (B::FEW) shared_few_rows<D, B::NC, B::WR, SHARED_WAVES, B::Q8, OWN>(a, run, tile, *(typename B::FewLds*)lds);
-  else shared_row_tiles<D, B::NC, B::Q8, OWN>(a, run, tile, *(SharedTilesLds<D, B::NC>*)lds);
+  else shared_row_tiles<D, B::Q8, OWN>(a, run, tile, *(SharedTilesLds<D>*)lds);
 }
 // Four wavefronts: with eight (128 keys, tails of 64) 8.7 us instead of 7.6 at 8 workgroups, 15.1 instead of 9.5 at 512
 #define SHARED_ALONE 4
