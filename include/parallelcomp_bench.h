@@ -29,7 +29,8 @@ typedef enum pc_kernel_id {
   PC_KERNEL_CHUNK_QUEUE = 18, PC_KERNEL_FP8_IMAGES = 19, PC_KERNEL_FP8_ROWS = 20,
   PC_KERNEL_SHARED_PREFIX = 21, PC_KERNEL_SHARED_TAIL = 22, PC_KERNEL_SHARED_MERGE = 23, PC_KERNEL_ROW8_APPEND = 24,
   PC_KERNEL_ROW8_READ = 25, PC_KERNEL_VERIFY_RACE = 26, PC_KERNEL_VERIFY_PICK = 27,
-  PC_KERNEL_COUNT = 28
+  PC_KERNEL_SHARED_ALONE = 28, PC_KERNEL_VERIFY_ALONE = 29,   /* the one-launch forms */
+  PC_KERNEL_COUNT = 30
 } pc_kernel_id;
 int         pc_profile_begin(void);
 int         pc_profile_begin_kernel(int kernel_id);   /* as pc_profile_begin, but only the launches of one

@@ -72,7 +72,8 @@ extern "C" const char* pc_kernel_name(int id) {
       "self_info_rows_kernel", "kv_append_kernel", "scores_lse_kernel", "kv_quantize_fp8_kernel",
       "decode_attn_fp8_kernel", "scores_kernel<1>+kv_prepass", "chunk_queue_kernel",
       "fp8_images_kernel", "fp8_rows_kernel", "shared_rows_kernel (prefix)", "shared_rows_kernel (tails)",
-      "shared_merge_kernel", "append_row8_kernel", "read_row8_kernel", "verify_race_kernel", "verify_pick_kernel"};
+      "shared_merge_kernel", "append_row8_kernel", "read_row8_kernel", "verify_race_kernel", "verify_pick_kernel",
+      "shared_alone_kernel", "verify_alone_kernel"};
   return (id >= 0 && id < PC_KERNEL_COUNT) ? names[id] : "unknown";
 }
 

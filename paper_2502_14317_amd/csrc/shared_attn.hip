@@ -1151,7 +1151,7 @@ static int launch_alone(const PcSharedCall& c, const SharedArgs& p, const Shared
 }
 template <int D>
 static int launch_alone_of(const PcSharedCall& c, const SharedArgs& p, const SharedArgs& t, hipStream_t st) {
-  PcProfScope prof(PC_KERNEL_SHARED_TAIL, st);
+  PcProfScope prof(PC_KERNEL_SHARED_ALONE, st);
   const long long n = (long long)c.batch * c.n_kv_heads;
   const int prefix = alone_formats(c).prefix;
   return prefix == 0 ? launch_alone<D, 0>(c, p, t, n, st) : (prefix == 1 ? launch_alone<D, 1>(c, p, t, n, st) : launch_alone<D, 2>(c, p, t, n, st));

@@ -191,7 +191,7 @@ int pc_launch_verify(const PcVerifyCall& c, void* ws, hipStream_t st) {
   x.parts = verify_parts(c.batch, c.vocab);
   x.per_part = ((c.vocab + x.parts - 1) / x.parts + 3) / 4 * 4;
   if (verify_alone(c.batch, c.vocab)) {
-    PcProfScope prof(PC_KERNEL_VERIFY_PICK, st);
+    PcProfScope prof(PC_KERNEL_VERIFY_ALONE, st);
     hipLaunchKernelGGL(verify_alone_kernel, dim3((unsigned)c.batch), dim3(1024), 0, st, x);
     PC_LAUNCH_CHECK();
     return PC_OK;
