@@ -986,8 +986,8 @@ static double time_of(double one_p, int np, double one_t, int nt) {
   const int rest = np & 255, room = 256 - rest;
   const double us = (np >> 8) * one_p, last = rest ? one_p : 0.0;
   if (nt == 0) return us + last;
-  const int beside = rest ? (int)(one_p / (1.4 * one_t)) * room : 0;     // tails that are surely done next to the last prefix ones
-  if (nt > beside && nt > room) return us + last + ((nt - beside + 255) >> 8) * one_t;
+  const double beside = rest ? floor(one_p / (1.4 * one_t)) * room : 0.0;      // tails that are surely done next to the last prefix ones
+  if (nt > beside && nt > room) return us + last + ((nt - (int)beside + 255) >> 8) * one_t;
   const double t_us = ((nt + room - 1) / room) * one_t;
   return us + (t_us > last ? t_us : last);
 }
