@@ -16,8 +16,9 @@
 // Measured (8 KV heads of 128 values): 64 rows, 8 x 2048 keys, 16 tails of 512: 26 us (the loop at 28 GB/s a CU, then starts and
 // the merge); 64 rows, 32 x 2048 keys of 8 bits 49 us; 4096 rows, 8 x 2048 keys 335 us (0.83 PFLOP/s); 4 rows, 128 keys 7.0 us.
 // Rows of 8 bits: a code is a bf16 value exactly, the key's scale multiplies the logit in fp32, the value's scale the
-// probability in front of its rounding.  Rotated query rows keep two bf16 parts (2^-17), in row tiles one (2^-9: the
-// second would take LDS that the keys have).
+// probability in front of its rounding.  Rotated query rows keep two bf16 parts (2^-17).  Probabilities are rounded to bf16 once
+// (up to 2^-8 of each, 1.7e-3 of the result's norm on average, as much as the result's own rounding): a second part would
+// double the second product.
 #include "decode_core.h"
 #include "serve.h"
 
@@ -98,8 +99,8 @@ __device__ __forceinline__ SharedBlock shared_block(const SharedArgs& a, const S
   return b;
 }
 
-// The tile's N query rows into LDS (rows behind the last one: zeros), rotated.  A rotated row is kept as two bf16 parts
-// where there is room for `lo`: their sum is the row to 2^-17.  D / 16 threads a row, 8 values of each half; every load
+// The tile's N query rows into LDS (rows behind the last one: zeros), rotated.  A rotated row is kept as two bf16 parts, whose
+// sum is the row to 2^-17 (`lo` is nullptr only where rows arrive rotated).  D / 16 threads a row, 8 values of each half; every load
 // is asked for in front of the arithmetic (`begin`), which has the first keys in flight behind it.
 template <int D, int N, int WAVES>
 struct SharedQueryRows {
@@ -632,17 +633,21 @@ struct SharedTile {
   float scale[2][SHARED_BLOCKS][32];                // [keys, values][block]
 };
 #define SHARED_TILE_ROWS (SHARED_WAVES * 32)
-template <int D>
+template <int D, int PARTS>
 struct SharedTilesLds {
   union {
     SharedTile<D> tile[2];
-    uint16_t q[SHARED_TILE_ROWS][D + 8];
+    uint16_t q[PARTS][SHARED_TILE_ROWS][D + 8];
   };
 };
 
-template <int D, bool Q8, bool OWN>
-__device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, int tile, SharedTilesLds<D>& sm) {
-  constexpr int KSTEPS = D / 32, VE = D / 16, ELEM = Q8 ? 1 : 2, ROW = D * ELEM, NC = 2, KB = 2;
+// PARTS: bf16 parts of a query row, two where it is rotated.  The second one's products and registers cost (4096 rows, 16384
+// keys) 340 -> 433 us, with 8-bit rows 422 -> 474; without it the result's error is 2.9e-3 of its norm instead of 2.3e-3 where
+// logits have a deviation of 1, and grows with that.  With 128 values a row, one block at a time then: two blocks' logits
+// beside both parts spill (452 and 504 us).
+template <int D, bool Q8, bool OWN, int PARTS>
+__device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, int tile, SharedTilesLds<D, PARTS>& sm) {
+  constexpr int KSTEPS = D / 32, VE = D / 16, ELEM = Q8 ? 1 : 2, ROW = D * ELEM, NC = 2, KB = PARTS == 2 && D == 128 ? 1 : 2;
   typedef uint32_t piece_t __attribute__((ext_vector_type(VE * ELEM / 4)));
   const int lane = threadIdx.x % PC_WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PC_WAVE);
   const int kk = lane / 16, c16 = lane % 16;
@@ -721,13 +726,15 @@ __device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, i
   rows.begin(a, x, threadIdx.x);
   SharedBlock last = shared_block(a, x, pc_blocks_begin<1>(lens, x.part, a.n_parts, a.parts_div, 0, lane, first_lens));
   Left at = issue(pieces, last);                            // the tile at hand
-  rows.finish(a, x, sm.q, nullptr, threadIdx.x);
+  rows.finish(a, x, sm.q[0], PARTS == 2 ? sm.q[PARTS - 1] : nullptr, threadIdx.x);
   PC_LDS_BARRIER();
-  bf16x8 bq[NC][KSTEPS];
+  bf16x8 bq[PARTS][NC][KSTEPS];
 #pragma unroll
-  for (int nc = 0; nc < NC; ++nc)
+  for (int h = 0; h < PARTS; ++h)
 #pragma unroll
-    for (int ks = 0; ks < KSTEPS; ++ks) bq[nc][ks] = *(const bf16x8*)&sm.q[16 * (wave * NC + nc) + c16][32 * ks + 8 * kk];
+    for (int nc = 0; nc < NC; ++nc)
+#pragma unroll
+      for (int ks = 0; ks < KSTEPS; ++ks) bq[h][nc][ks] = *(const bf16x8*)&sm.q[h][16 * (wave * NC + nc) + c16][32 * ks + 8 * kk];
   PC_LDS_BARRIER();
   int unseen[NC];
 #pragma unroll
@@ -743,7 +750,7 @@ __device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, i
   }
 
   // KB blocks together, so that their chains overlap; a block behind the run's end has no keys.  The products go first where
-  // both wavefronts of a SIMD can issue (4096 rows, 16384 keys: 341 -> 333 us).
+  // both wavefronts of a SIMD can issue (4096 rows as they arrive, 16384 keys: 341 -> 335 us).
   auto consume = [&](const SharedTile<D>& t, int first, const int (&left)[KB]) __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(1);
     floatx4 s[NC][KB][2];
@@ -754,16 +761,22 @@ __device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, i
 #pragma unroll
         for (int bi = 0; bi < 2; ++bi) s[nc][b][bi] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int ks = 0; ks < KSTEPS; ++ks)
+    for (int ks = 0; ks < KSTEPS; ++ks) {
+      u32x4 ka[KB][2];
 #pragma unroll
       for (int b = 0; b < KB; ++b)
 #pragma unroll
-        for (int bi = 0; bi < 2; ++bi) {
-          const u32x4 ka = t.k[first + b][bi][ks][lane];
+        for (int bi = 0; bi < 2; ++bi) ka[b][bi] = t.k[first + b][bi][ks][lane];
 #pragma unroll
-          for (int nc = 0; nc < NC; ++nc)
-            s[nc][b][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)&ka, bq[nc][ks], s[nc][b][bi], 0, 0, 0);
-        }
+      for (int h = PARTS - 1; h >= 0; --h)                   // (a sum's two parts are four products apart)
+#pragma unroll
+        for (int b = 0; b < KB; ++b)
+#pragma unroll
+          for (int bi = 0; bi < 2; ++bi)
+#pragma unroll
+            for (int nc = 0; nc < NC; ++nc)
+              s[nc][b][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)&ka[b][bi], bq[h][nc][ks], s[nc][b][bi], 0, 0, 0);
+    }
     SharedScales sc[KB];
     if constexpr (Q8) {
 #pragma unroll
@@ -793,8 +806,15 @@ __device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, i
   Left ahead = issue(pieces, last);                         // the one on its way
   PC_LDS_BARRIER();
   for (int buf = 0; at.b0 > 0; buf ^= 1) {
-    consume(sm.tile[buf], 0, {at.b0, at.b1});
-    if (at.b2 > 0) consume(sm.tile[buf], 2, {at.b2, at.b3});
+    if constexpr (KB == 2) {
+      consume(sm.tile[buf], 0, {at.b0, at.b1});
+      if (at.b2 > 0) consume(sm.tile[buf], 2, {at.b2, at.b3});
+    } else {
+      consume(sm.tile[buf], 0, {at.b0});
+      if (at.b1 > 0) consume(sm.tile[buf], 1, {at.b1});
+      if (at.b2 > 0) consume(sm.tile[buf], 2, {at.b2});
+      if (at.b3 > 0) consume(sm.tile[buf], 3, {at.b3});
+    }
     commit(buf ^ 1, pieces);
     at = ahead;
     last = next(last);
@@ -905,15 +925,17 @@ __global__ __launch_bounds__(256) void shared_merge_kernel(SharedMergeArgs a) {
 }
 
 // ------------------------------------------------------------------------------------------ launches
-// What a launch's workgroups are: few rows (16, 32 or 64 of them), row tiles of 256 rows; odd numbers: 8-bit rows
-enum SharedBody { SHARED_FEW16 = 2, SHARED_FEW32 = 4, SHARED_FEW64 = 6, SHARED_TILE = 8 };
+// What a launch's workgroups are: few rows (16, 32 or 64 of them), row tiles of 256 rows, those of rotated rows (the launch
+// sees to it: a plan has SHARED_TILE); odd numbers: 8-bit rows
+enum SharedBody { SHARED_FEW16 = 2, SHARED_FEW32 = 4, SHARED_FEW64 = 6, SHARED_TILE = 8, SHARED_TILE_ROTATED = 10 };
 static constexpr int shared_body_rows(int body) { return body >= SHARED_TILE ? SHARED_TILE_ROWS : 8 << body / 2; }
 template <int D, int BODY>
 struct SharedBodyOf {
   static constexpr bool Q8 = BODY % 2, FEW = BODY < SHARED_TILE;
   static constexpr int ROWS = shared_body_rows(BODY), NC = ROWS < 32 ? 1 : 2, WR = FEW ? ROWS / (16 * NC) : 1;
+  static constexpr int PARTS = BODY >= SHARED_TILE_ROTATED ? 2 : 1;
   typedef SharedFewLds<D, NC, WR, SHARED_WAVES> FewLds;
-  static constexpr int LDS = FEW ? sizeof(FewLds) : sizeof(SharedTilesLds<D>);
+  static constexpr int LDS = FEW ? sizeof(FewLds) : sizeof(SharedTilesLds<D, PARTS>);
 };
 // Partials of `a`'s keys: OWN, of tails; else of prefixes, and behind their n_first workgroups those of the tails of up
 // to 16 rows.  An XCD (number mod 8) has an eighth of (run, tile), the tiles of a run behind each other: its L2 serves
@@ -931,7 +953,7 @@ __global__ __launch_bounds__(SHARED_THREADS, 2) void shared_rows_kernel(SharedAr
   if (at >= a.n_runs * a.n_tiles) return;
   const int run = pc_div(at, a.tiles_div), tile = at - run * a.n_tiles;
   if constexpr (B::FEW) shared_few_rows<D, B::NC, B::WR, SHARED_WAVES, B::Q8, OWN>(a, run, tile, *(typename B::FewLds*)lds);
-  else shared_row_tiles<D, B::Q8, OWN>(a, run, tile, *(SharedTilesLds<D>*)lds);
+  else shared_row_tiles<D, B::Q8, OWN, B::PARTS>(a, run, tile, *(SharedTilesLds<D, B::PARTS>*)lds);
 }
 // Four wavefronts: with eight (128 keys, tails of 64) 8.7 us instead of 7.6 at 8 workgroups, 15.1 instead of 9.5 at 512
 #define SHARED_ALONE 4
@@ -957,7 +979,7 @@ static PcSharedSide side_of(long long n_caches, long long rows, int n_kv_heads, 
 // or a block's latencies; queries, partials and latencies 5.5 to 10 us a workgroup (64 values a row: 0.6 of that)
 static SharedCost cost_of(const PcSharedSide& s, const PcRows& r, int D, double share) {
   static const struct { double start, bf16, row8, least; } of[] = {      // us, TFLOP/s, TFLOP/s, us
-      {5.5, 2.6, 2.0, 0.0}, {6.5, 1.8, 3.0, 0.0}, {7.5, 2.5, 2.3, 0.35}, {10.0, 3.0, 2.4, 1.1}};
+      {5.5, 2.6, 2.0, 0.0}, {6.5, 1.8, 3.0, 0.0}, {7.5, 2.5, 2.3, 0.35}, {10.0, 2.3, 2.1, 1.4}};
   const auto& m = of[s.body / 2 - 1];
   SharedCost c = {};
   c.bytes = block_bytes(r, D);
@@ -1129,7 +1151,7 @@ static int launch(const SharedArgs& a, const SharedArgs& tail, long long n, long
 template <int D, bool OWN>
 static int launch_rows(const PcSharedSide& s, const SharedArgs& a, const SharedArgs& tail, long long n_tail, hipStream_t st) {
   const long long n = workgroups(s);
-  switch (s.body) {
+  switch (s.body >= SHARED_TILE && a.q_pos ? s.body + SHARED_TILE_ROTATED - SHARED_TILE : s.body) {
     case SHARED_FEW16: return launch<D, SHARED_FEW16, OWN>(a, tail, n, n_tail, st);
     case SHARED_FEW16 + 1: return launch<D, SHARED_FEW16 + 1, OWN>(a, tail, n, n_tail, st);
     case SHARED_FEW32: return launch<D, SHARED_FEW32, OWN>(a, tail, n, n_tail, st);
@@ -1138,6 +1160,8 @@ static int launch_rows(const PcSharedSide& s, const SharedArgs& a, const SharedA
     case SHARED_FEW64 + 1: return launch<D, SHARED_FEW64 + 1, OWN>(a, tail, n, n_tail, st);
     case SHARED_TILE: return launch<D, SHARED_TILE, OWN>(a, tail, n, n_tail, st);
     case SHARED_TILE + 1: return launch<D, SHARED_TILE + 1, OWN>(a, tail, n, n_tail, st);
+    case SHARED_TILE_ROTATED: return launch<D, SHARED_TILE_ROTATED, OWN>(a, tail, n, n_tail, st);
+    case SHARED_TILE_ROTATED + 1: return launch<D, SHARED_TILE_ROTATED + 1, OWN>(a, tail, n, n_tail, st);
     default: return PC_OK;                                   // no such rows
   }
 }
