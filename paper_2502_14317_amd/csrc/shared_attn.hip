@@ -10,7 +10,9 @@
 //              registers, a key read by as many wavefronts as there are groups of 32 rows;
 //   row tiles  (256 rows): a wavefront has 32 rows; tiles of 128 keys go through LDS as matrix operands, widened and
 //              transposed once on the way in, so that every wavefront reads them with 16 consecutive bytes a lane;
-//   tails      of up to 16 rows: one to eight wavefronts each, behind the prefix's workgroups in their launch.
+//   tails      of up to 16 rows: one to eight wavefronts each, behind the prefix's workgroups in their launch; of more rows
+//              the same bodies in a launch of their own, where 128 values spill 23 to 77 registers (32 columns' state beside
+//              the path for values that are not finite).
 // Where few keys are shared, one launch takes every (sequence, KV head) for itself, prefix and tail (shared_alone).
 // Bound by memory up to some 170 rows (8-bit rows: 85), by the matrix cores and the softmax's vector instructions beyond.
 // Measured (8 KV heads of 128 values): 64 rows, 8 x 2048 keys, 16 tails of 512: 26 us (the loop at 28 GB/s a CU, then starts and
@@ -976,27 +978,28 @@ static PcSharedSide side_of(long long n_caches, long long rows, int n_kv_heads, 
   return s;
 }
 // Measured, one workgroup a CU: 27 GB/s of keys a CU; or the arithmetic, rows x keys of a block at 1.8 to 3.0 TFLOP/s a CU,
-// or a block's latencies; queries, partials and latencies 5.5 to 10 us a workgroup (64 values a row: 0.6 of that)
+// or a block's latencies (64 values a row: half); queries, partials and latencies 5.5 to 12 us a workgroup (0.6 of that).
+// Tails in a launch of their own are priced as prefixes are
 static SharedCost cost_of(const PcSharedSide& s, const PcRows& r, int D, double share) {
   static const struct { double start, bf16, row8, least; } of[] = {      // us, TFLOP/s, TFLOP/s, us
-      {5.5, 2.6, 2.0, 0.0}, {6.5, 1.8, 3.0, 0.0}, {7.5, 2.5, 2.3, 0.35}, {10.0, 2.3, 2.1, 1.4}};
+      {5.5, 2.6, 2.0, 0.0}, {6.5, 1.8, 3.0, 0.0}, {7.5, 2.5, 2.3, 0.35}, {12.0, 2.7, 1.9, 1.7}};
   const auto& m = of[s.body / 2 - 1];
   SharedCost c = {};
   c.bytes = block_bytes(r, D);
   const double memory = c.bytes / 27e3, arithmetic = 4.0 * 32 * shared_body_rows(s.body) * D / ((r.k_scale ? m.row8 : m.bf16) * 1e6);
   c.start = m.start * (D == 64 ? 0.6 : 1.0);
-  c.block = fmax(fmax(memory, arithmetic), m.least);
+  c.block = fmax(fmax(memory, arithmetic), m.least * (D == 64 ? 0.5 : 1.0));
   c.blocks = blocks_of(r, share) + 1.0;
   c.most = c.blocks < 8.0 ? 1 : (c.blocks > 256.0 ? 64 : (int)(c.blocks / 4.0));
   return c;
 }
-// One launch, a workgroup of four wavefronts a (sequence, KV head): prefix keys at 58 GB/s a CU (they are in its L2), the
-// tail's at 28, or a block's latency
+// One launch, a workgroup of four wavefronts a (sequence, KV head), as many a CU as the fullest one has: prefix keys at 55 GB/s
+// a CU (they are in its L2), the tail's at 31, or a block's latency.  380 such calls: 8 % off (root mean square)
 static double alone_us(const PcSharedCall& c) {
-  const double a_cu = (double)c.batch * c.n_kv_heads / 256.0, at_once = a_cu < 1.0 ? 1.0 : a_cu;
+  const double a_cu = (double)c.batch * c.n_kv_heads / 256.0, at_once = ceil(a_cu);
   const double p = blocks_of(c.prefix, 1.0), t = blocks_of(c.tail, 0.75) + 1.0;
-  return 5.7 + 0.7 * a_cu + fmax(at_once * p * block_bytes(c.prefix, c.head_dim) / 58e3, 0.13 * p) +
-         fmax(at_once * t * block_bytes(c.tail, c.head_dim) / 28e3, 0.23 * t);
+  return 5.7 + 0.7 * a_cu + fmax(at_once * p * block_bytes(c.prefix, c.head_dim) / 55e3, 0.13 * p) +
+         fmax(at_once * t * block_bytes(c.tail, c.head_dim) / 31e3, 0.2 * t);
 }
 // A workgroup of 8 / waves tails' runs: the CU's reads, or a wavefront's blocks one after the other
 static double tails_us(const SharedCost& c, int waves, int tp) {
@@ -1054,13 +1057,15 @@ static double cut_of(const PcSharedCall& c, PcSharedPlan& p) {
   }
   return least;
 }
-// Of the bodies that fit, and of one launch for all (up to 16 rows), the one of least estimated time.  688 calls of 32 to 4096
-// rows a KV head and 512 to 16384 keys (both formats, 64 and 128 values) were timed with each body, and in one launch where
-// that is possible: the choice costs 2 % over the best on average (7 % at the 90th percentile); 64 rows at up to 128 and tiles
-// beyond, by the number of rows alone, cost 13 %; one launch at up to 512 keys, 15 % where it is possible (now 1 %).  us with
-// 32 rows / 64 rows / tiles, bf16: (64 rows x 1024 keys) 13.8 / 16.0 / 18.9, (512 x 1024) 26 / 19.5 / 31, (512 x 16384) 109 / 96
-// / 82, (4096 x 16384) 761 / 606 / 316; 8 bits: (64 x 1024) 13.8 / 15.9 / 20, (512 x 16384) 74 / 77 / 91, (4096 x 16384) 475 /
-// 439 / 412.  One launch / two: (16 sequences, 128 keys, tails of 64) 7.8 / 13.7, (16, 1024, 64) 14.9 / 15.2, (4, 1024, 512) 20 / 14.
+// Of the bodies that fit, and of one launch for all (up to 16 rows), the one of least estimated time, rows taken as rotated (the
+// plan does not know).  600 calls with tails of up to 16 rows (2 to 4096 rows a KV head, 60 to 32768 keys, both formats, 64 and
+// 128 values) and 200 with tails of more were timed with each body.  The choice costs 2 % and 4 % over the best in the mean, 9 and
+// 17 % at the 90th percentile, 33 and 65 % at most; one launch throughout 61 % more than it, 32 rows 9 and 3 %, 64 rows 8 and
+// 3 %, tiles 33 and 14 %.  us with 32 rows / 64 rows / tiles, bf16: (64 rows x 1024 keys) 13.2 / 15.2 / -, (512 x 1024) 22.8 / 22.7 /
+// 32.4, (512 x 16384) 110 / 94 / 87, (4096 x 16384) 840 / 605 / 407; 8 bits: (64 x 1024) 13.4 / 15.1 / -, (512 x 16384) 74 / 71 / 90,
+// (4096 x 16384) 478 / 438 / 451.  One launch / two: (16 sequences, 128 keys, tails of 64) 7.6 / 11.2, (16, 1024, 64) 14.6 / 12.9,
+// (4, 1024, 512) 20.1 / 13.9.  Tails, 8 x 2048 keys in front: (16 sequences, 64 rows, 512) 151 / 152 / -, (16, 256, 512) 493 / 461 /
+// 430, (4, 1200, 600) 673 / 644 / 586.
 PcSharedPlan pc_shared_plan(const PcSharedCall& c) {
   const long long own_rows = (long long)c.n_q * (c.n_q_heads / c.n_kv_heads), rows = c.batch / c.n_prefix * own_rows;
   auto bodies = [](long long n, int (&of)[3]) {

@@ -56,7 +56,12 @@ CASES = [
     (34, 1, 17, 14, 2, 128, 1, 195, 169, "bf16", "row8"),
     (6, 1, 354, 6, 2, 64, 2, 102, 55, "row8", "row8"),
     (31, 1, 37, 8, 4, 64, 3, 100, 77, "row8", "row8"),
+    (69, 1, 17, 8, 2, 64, 2, 97, 25, "row8", "row8"),
+    (51, 1, 17, 8, 2, 128, 3, 55, 26, "row8", "row8"),
     # tails alone
+    (2, 1, 1, 2, 2, 64, 0, 1, 1300, "bf16", "bf16"),
+    (3, 1, 1, 2, 2, 64, 0, 1, 1700, "row8", "row8"),
+    (3, 3, 1, 2, 2, 128, 0, 1, 2300, "row8", "row8"),
     (2, 1, 1, 2, 1, 64, 0, 1, 727, "row8", "bf16"),
     (1, 1, 1, 4, 1, 64, 0, 1, 833, "row8", "row8"),
     (1, 1, 2, 2, 2, 128, 0, 1, 903, "bf16", "bf16"),
