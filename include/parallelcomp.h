@@ -405,7 +405,7 @@ typedef struct pc_row_cache {
  *                                U { tail[b, g, j], j < visible } of q . k * scale, times the values
  * A key of a prefix is read from memory once for the query rows of all F sequences.
  *   q [B, n_q, H_q, D] bf16; q_pos [B] int32 (device), nullable: row t is rotated here at position
- *     pos0 + q_pos[b] + t >= 0 (then kept to bf16 or better), so that the tails' lengths in front of the step serve
+ *     pos0 + q_pos[b] + t >= 0 (in fp32, kept to 2^-17 as two bf16 parts), so that the tails' lengths in front of the step serve
  *     as q_pos, with pos0 the position of a tail's first row; NULL: q arrives rotated.
  *   prefix: rows of n = n_prefix; NULL for none.   tail: rows of n = batch with n_seg = 1; NULL for none.
  *     n_seg = 0 is none, too: its pointers are not looked at.
@@ -417,7 +417,7 @@ typedef struct pc_row_cache {
  * Whatever lies in rows behind the lengths, and in rows that a query row does not see, stays out of its result,
  * infinities and NaN included.
  * Arithmetic: bf16 MFMA products (8-bit codes widened exactly), logits scaled in fp32, fp32 softmax and
- * accumulation, probabilities (times the row's V scale) rounded to bf16 for the second product.
+ * accumulation, probabilities (at most 1; times the row's V scale) rounded to bf16 once for the second product.
  * batch, n_q, n_seg, H_q up to 2^20 each, cap up to 2^24, B n_q H_q < 2^25; PC_ERR_SHAPE otherwise.
  * Workspace: pc_shared_attn_workspace_bytes(...) of the same sizes and formats. */
 int pc_shared_attn(const void* q, const int32_t* q_pos, int32_t pos0, float rope_base, float softmax_scale,

@@ -16,7 +16,8 @@
 // Where few keys are shared, one launch takes every (sequence, KV head) for itself, prefix and tail (shared_alone).
 // Bound by memory up to some 170 rows (8-bit rows: 85), by the matrix cores and the softmax's vector instructions beyond.
 // Measured (8 KV heads of 128 values): 64 rows, 8 x 2048 keys, 16 tails of 512: 26 us (the loop at 28 GB/s a CU, then starts and
-// the merge); 64 rows, 32 x 2048 keys of 8 bits 49 us; 4096 rows, 8 x 2048 keys 335 us (0.83 PFLOP/s); 4 rows, 128 keys 7.0 us.
+// the merge); 64 rows, 32 x 2048 keys of 8 bits 48 us; 4096 rows, 8 x 2048 keys 430 us (0.65 PFLOP/s), 322 as they arrive; 4 rows,
+// 128 keys 7.0 us.
 // Rows of 8 bits: a code is a bf16 value exactly, the key's scale multiplies the logit in fp32, the value's scale the
 // probability in front of its rounding.  Rotated query rows keep two bf16 parts (2^-17).  Probabilities are rounded to bf16 once
 // (up to 2^-8 of each, 1.7e-3 of the result's norm on average, as much as the result's own rounding): a second part would
@@ -752,7 +753,8 @@ __device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, i
   }
 
   // KB blocks together, so that their chains overlap; a block behind the run's end has no keys.  The products go first where
-  // both wavefronts of a SIMD can issue (4096 rows as they arrive, 16384 keys: 341 -> 335 us).
+  // both wavefronts of a SIMD can issue (4096 rows as they arrive, 16384 keys: 335 -> 322 us; rotated ones 429 -> 434, 8-bit rows 448
+  // -> 442).
   auto consume = [&](const SharedTile<D>& t, int first, const int (&left)[KB]) __attribute__((always_inline)) {
     __builtin_amdgcn_s_setprio(1);
     floatx4 s[NC][KB][2];
