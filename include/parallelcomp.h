@@ -417,7 +417,9 @@ typedef struct pc_row_cache {
  * Whatever lies in rows behind the lengths, and in rows that a query row does not see, stays out of its result,
  * infinities and NaN included.
  * Arithmetic: bf16 MFMA products (8-bit codes widened exactly), logits scaled in fp32, fp32 softmax and
- * accumulation, probabilities (at most 1; times the row's V scale) rounded to bf16 once for the second product.
+ * accumulation, probabilities (at most 1; times the row's V scale) rounded to bf16 once for the second product.  So sums stay
+ * in fp32's range wherever those of a softmax relative to the row's maximum do; values of 8-bit rows below 2^-110 lose bits
+ * (a probability times its scale is subnormal), 16-bit ones keep theirs.
  * batch, n_q, n_seg, H_q up to 2^20 each, cap up to 2^24, B n_q H_q < 2^25; PC_ERR_SHAPE otherwise.
  * Workspace: pc_shared_attn_workspace_bytes(...) of the same sizes and formats. */
 int pc_shared_attn(const void* q, const int32_t* q_pos, int32_t pos0, float rope_base, float softmax_scale,
