@@ -473,6 +473,103 @@ int pc_verify_drafts(const int32_t* draft, const int32_t* draft_len, const float
                      const int32_t* len_in, int32_t* len_out, void* ws, size_t ws_bytes, void* stream);
 size_t pc_verify_drafts_workspace_bytes(int32_t batch, int32_t n_draft, int32_t vocab);
 
+/* ---- drafted trees over a paged cache, and what tokens are worth (extension) -------------------
+ * Serving sequences of very unequal lengths: keys and values lie in pages of a pool, and row j of sequence b (any row,
+ * document or answer) is row j % page of page table[b, j / page].
+ *   k, v     [n_pages, H_kv, page, D] bf16 with both scales NULL; or OCP E4M3 codes (one byte a value) with one fp32 scale
+ *            a row, value = code * scale, rounded as pc_kv_append_row8 rounds
+ *   table    [B, max_pages] int32 (device).  A number outside [0, n_pages) is no page, and there is none behind the last:
+ *            its rows are not there, i.e. nothing is written to them, nobody sees them.  Sequences may share pages, but no
+ *            row that a call writes is another sequence's, too.
+ *   page     16, 32, .. 65536 rows (a power of two); max_pages * page up to 2^30.
+ * n_pages up to 2^31 - 1; the pool may be larger than 4 GiB. */
+typedef struct pc_page_cache {
+  void*          k;                /* 16-byte aligned                                                 */
+  void*          v;
+  float*         k_scale;          /* [n_pages, H_kv, page] fp32, both or neither                     */
+  float*         v_scale;
+  const int32_t* table;
+  int32_t        n_pages;
+  int32_t        page;
+  int32_t        max_pages;
+} pc_page_cache;
+
+/* Trees.  A step's n rows of a sequence are the nodes of a tree of drafted tokens (or several trees): node t hangs below
+ * parent[b, t] < t, a root has -1 (every other value outside [0, t) makes a root, too).  parent [B, n] int32 (device), up
+ * to 64 nodes; NULL: a chain, node t below node t - 1.  Node t's depth is the number of nodes above it, and its position
+ * pos0 + pos[b] + depth, which must be in [0, 2^31): siblings stand at the same one.
+ * n_rows [B] int32 (device), nullable (all n): the first n_rows[b] nodes (clamped to [0, n]) are sequence b's; what belongs
+ * to others is neither read into a result nor written.
+ *
+ * Append: the rows of n_new nodes, or of as many following tokens (parent NULL: any n_new), behind the len_in[b] that
+ * the sequence holds; keys rotated on the way (pos != NULL) and rounded once, bf16 or 8 bits by the cache's format.
+ *   k_new, v_new bf16, row (b, t, g) at b * batch_stride + t * row_stride + g * head_stride elements (all three the same
+ *   for both, multiples of 8; all zero: [B, n_new, H_kv, D] contiguous), as one projection leaves q, k and v, or a gather
+ *   its segments.  A row that holds an infinity or a NaN reads back as NaN from 8 bits.
+ *   pos [B] int32 (device), nullable (keys arrive rotated; rope_base is not looked at)
+ *   len_in [B] int32 (device), nullable (all 0; at least 0); len_out [B], nullable: len_in + n_rows, whether the rows are
+ *   there or not.  They must not overlap: each of a sequence's workgroups reads len_in.
+ * B * n_new * H_kv < 2^31.  No workspace. */
+int pc_kv_append_paged(const void* k_new, const void* v_new, int64_t batch_stride, int64_t row_stride, int64_t head_stride,
+                       const int32_t* parent, const int32_t* n_rows, const int32_t* pos, int32_t pos0, float rope_base,
+                       int32_t batch, int32_t n_new, int32_t n_kv_heads, int32_t head_dim, const pc_page_cache* cache,
+                       const int32_t* len_in, int32_t* len_out, void* stream);
+
+/* Attention of a tree's nodes over their sequence's pages: with base = len[b] - n_rows[b] (the nodes' rows are appended
+ * first and are the last of the sequence), node t sees
+ *   the rows j < base, its own row base + t, and the rows base + u of every node u above it,
+ * all under one softmax.  n = 1 is a decoding step.
+ *   q bf16, row (b, t, h) at b * batch_stride + t * row_stride + h * D elements (multiples of 8; both zero: [B, n, H_q, D]
+ *   contiguous); pos [B] int32 (device): rotated here at the nodes' positions (kept to 2^-17 as two bf16 parts); NULL: q
+ *   arrives rotated.   len [B] int32 (device).
+ *   out [B, n, H_q, D] bf16; a row that sees nothing is 0.  lse_out [B, H_q, n] fp32, nullable (natural log; -inf there).
+ * Whatever lies in rows that a node does not see stays out of its result, infinities and NaN included.
+ * Arithmetic as pc_shared_attn's: bf16 MFMA products (8-bit codes widened exactly), logits, softmax and sums in fp32,
+ * probabilities (at most 1; times the row's V scale) rounded to bf16 once.  The way a sequence's rows are cut, and with
+ * it the last bits of its result, depends on the lengths of the whole batch; the same call gives the same bits.
+ * H_q up to 2^20, batch up to 2^20, B n H_q < 2^25, B max_pages page < 2^36.  Workspace: pc_tree_attn_workspace_bytes(...) of the same sizes: it does
+ * not depend on lengths, so that a captured call stays valid as they grow. */
+int pc_tree_attn(const void* q, int64_t batch_stride, int64_t row_stride, const int32_t* parent, const int32_t* n_rows,
+                 const int32_t* pos, int32_t pos0, float rope_base, float softmax_scale, const pc_page_cache* cache,
+                 const int32_t* len, int32_t batch, int32_t n, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
+                 void* out, float* lse_out, void* ws, size_t ws_bytes, void* stream);
+size_t pc_tree_attn_workspace_bytes(const pc_page_cache* cache, int32_t batch, int32_t n, int32_t n_q_heads,
+                                    int32_t n_kv_heads, int32_t head_dim);
+
+/* What the tokens of a vocabulary are worth: with p = softmax(logits[r, :]),
+ *   token_logprob[r, i] = log p(tokens[r, i]); NaN for a token outside [0, vocab)
+ *   entropy[r]          = -sum p log p (nats; terms of p = 0 are 0), nullable
+ *   top_idx[r, i]       = the n_top largest logits' tokens (logit descending, token ascending; NaN below everything, -0 = +0),
+ *   top_logprob[r, i]   = and their log p, nullable.
+ *   logits [rows, vocab] bf16 (logits_fp32 0) or fp32 (1), a row every row_stride >= vocab elements (0: vocab), at any
+ *   element boundary;  tokens [rows, n_tokens] int32 (device), n_tokens 0 .. 2^16 (0: tokens and token_logprob are not looked
+ *   at);  n_top 0 .. 64, at most vocab (0: top_idx and top_logprob are not looked at).
+ * A row that holds a NaN or +inf, or nothing but -inf, gives NaN for every number (top_idx as above).  fp32 sums in a fixed order
+ * (deterministic).  rows 0 .. 2^21, vocab 1 .. 2^24.  Workspace: pc_token_logprobs_workspace_bytes(rows, vocab, n_top). */
+int pc_token_logprobs(const void* logits, int32_t logits_fp32, int64_t row_stride, const int32_t* tokens, int32_t n_tokens,
+                      int32_t n_top, int32_t rows, int32_t vocab, float* token_logprob, float* entropy, int32_t* top_idx,
+                      float* top_logprob, void* ws, size_t ws_bytes, void* stream);
+size_t pc_token_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t n_top);
+
+/* Accept the path of a tree that the target follows.  Node 0 (the sequence's last token) stands if n_rows[b] > 0; below a
+ * standing node a, the lowest child c with tokens[b, c] == choice(b, a) stands, if there is one: choice is the target's own
+ * token behind node a (the most likely one, or one drawn from its distribution; then the answer is distributed as
+ * the target's).  The rows of the standing nodes move to base, base + 1, .. (base = len_in[b] - n_rows[b]), in both keys and
+ * values, so that the cache holds the answer's rows in a row.
+ *   tokens [B, n] int32; parent, n_rows as above; choice [B, n] int32, node (b, t) at (b * n + t) * choice_stride
+ *     (>= 1; n_top where it is top_idx of pc_token_logprobs)
+ *   path [B, n] int32 out: the standing nodes, then -1;  n_kept [B] out: their number;  next_token [B] out: the choice at the
+ *     last of them, -1 if there is none
+ *   cache: rows are moved; NULL: none (n_kv_heads, head_dim, len_in and len_out are not looked at).  A layer's call each; one of
+ *     them brings the lengths and positions up to date.
+ *   len_in [B] int32 (device): rows with the tree's; len_out [B], nullable: base + n_kept.  They must not overlap.
+ *   pos [B] int32 (device), nullable: n_kept is added in place.
+ * Rows that are not there are not moved.  n 1 .. 64, batch up to 2^20.  No workspace. */
+int pc_tree_accept(const int32_t* tokens, const int32_t* parent, const int32_t* choice, int32_t choice_stride,
+                   const int32_t* n_rows, int32_t batch, int32_t n, const pc_page_cache* cache, int32_t n_kv_heads,
+                   int32_t head_dim, const int32_t* len_in, int32_t* len_out, int32_t* pos, int32_t* path, int32_t* n_kept,
+                   int32_t* next_token, void* stream);
+
 /* ---- housekeeping -------------------------------------------------------------------------- */
 const char* pc_status_string(int status);   /* static string, never NULL                       */
 int         pc_last_hip_error(void);        /* hipError_t of the last PC_ERR_HIP on this thread */

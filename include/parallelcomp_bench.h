@@ -30,7 +30,9 @@ typedef enum pc_kernel_id {
   PC_KERNEL_SHARED_PREFIX = 21, PC_KERNEL_SHARED_TAIL = 22, PC_KERNEL_SHARED_MERGE = 23, PC_KERNEL_ROW8_APPEND = 24,
   PC_KERNEL_ROW8_READ = 25, PC_KERNEL_VERIFY_RACE = 26, PC_KERNEL_VERIFY_PICK = 27,
   PC_KERNEL_SHARED_ALONE = 28, PC_KERNEL_VERIFY_ALONE = 29,   /* the one-launch forms */
-  PC_KERNEL_COUNT = 30
+  PC_KERNEL_PAGED_APPEND = 30, PC_KERNEL_TREE_ATTN = 31, PC_KERNEL_TREE_MERGE = 32, PC_KERNEL_LOGPROBS = 33,
+  PC_KERNEL_LOGPROBS_JOIN = 34, PC_KERNEL_TREE_ACCEPT = 35,
+  PC_KERNEL_COUNT = 36
 } pc_kernel_id;
 int         pc_profile_begin(void);
 int         pc_profile_begin_kernel(int kernel_id);   /* as pc_profile_begin, but only the launches of one

@@ -13,4 +13,6 @@ from .binding import (lib, make_shape, alloc_workspace, pc_shape, PcError, SYMBO
                       pc_decode_step_fp8, pc_decode_step_fp8_workspace_bytes,
                       pc_row_cache, make_row_cache, pc_shared_attn, pc_shared_attn_workspace_bytes, pc_shared_attn_plan, pc_kv_append_row8,
                       pc_kv_read_row8, pc_verify_drafts, pc_verify_drafts_workspace_bytes,
+                      pc_page_cache, make_page_cache, pc_kv_append_paged, pc_tree_attn, pc_tree_attn_workspace_bytes,
+                      pc_token_logprobs, pc_token_logprobs_workspace_bytes, pc_tree_accept,
                       pc_profile_begin, pc_profile_end, pc_profile_records, pc_mfma_ceiling, pc_copy_ceiling)

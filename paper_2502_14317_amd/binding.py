@@ -7,7 +7,7 @@ There is no fallback: if the library is missing, loading raises.
 """
 import ctypes
 import os
-from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_size_t, c_void_p
+from ctypes import POINTER, Structure, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_void_p
 
 import torch
 
@@ -29,6 +29,8 @@ SYMBOLS = [
     "pc_decode_step_fp8_workspace_bytes", "pc_layer_forward", "pc_layer_workspace_bytes",
     "pc_shared_attn", "pc_shared_attn_workspace_bytes", "pc_kv_append_row8", "pc_kv_read_row8",
     "pc_verify_drafts", "pc_verify_drafts_workspace_bytes", "pc_shared_attn_plan",
+    "pc_kv_append_paged", "pc_tree_attn", "pc_tree_attn_workspace_bytes", "pc_token_logprobs",
+    "pc_token_logprobs_workspace_bytes", "pc_tree_accept",
 ]
 
 
@@ -46,6 +48,11 @@ class pc_row_cache(Structure):
 class pc_shared_attn_plan_info(Structure):
     _fields_ = [(name, c_int32) for name in ("alone", "prefix_format", "prefix_rows", "prefix_parts", "tail_format", "tail_rows",
                                              "tail_parts", "tail_waves", "tails_behind")]
+
+
+class pc_page_cache(Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p), ("table", c_void_p),
+                ("n_pages", c_int32), ("page", c_int32), ("max_pages", c_int32)]
 
 
 class PcError(RuntimeError):
@@ -154,6 +161,20 @@ def lib():
     L.pc_verify_drafts.restype = c_int
     L.pc_verify_drafts_workspace_bytes.argtypes = [c_int32] * 3
     L.pc_verify_drafts_workspace_bytes.restype = c_size_t
+    L.pc_kv_append_paged.argtypes = ([P, P] + [c_int64] * 3 + [P] * 3 + [c_int32, c_float] + [c_int32] * 4 + [POINTER(pc_page_cache)] +
+                                     [P] * 3)
+    L.pc_kv_append_paged.restype = c_int
+    L.pc_tree_attn.argtypes = ([P, c_int64, c_int64] + [P] * 3 + [c_int32, c_float, c_float, POINTER(pc_page_cache), P] + [c_int32] * 5 +
+                               [P, P, P, c_size_t, P])
+    L.pc_tree_attn.restype = c_int
+    L.pc_tree_attn_workspace_bytes.argtypes = [POINTER(pc_page_cache)] + [c_int32] * 5
+    L.pc_tree_attn_workspace_bytes.restype = c_size_t
+    L.pc_token_logprobs.argtypes = [P, c_int32, c_int64, P] + [c_int32] * 4 + [P] * 5 + [c_size_t, P]
+    L.pc_token_logprobs.restype = c_int
+    L.pc_token_logprobs_workspace_bytes.argtypes = [c_int32] * 3
+    L.pc_token_logprobs_workspace_bytes.restype = c_size_t
+    L.pc_tree_accept.argtypes = ([P] * 3 + [c_int32, P, c_int32, c_int32, POINTER(pc_page_cache), c_int32, c_int32] + [P] * 7)
+    L.pc_tree_accept.restype = c_int
     _lib = L
     return L
 
@@ -396,6 +417,51 @@ def make_row_cache(k, v, k_scale=None, v_scale=None, seg_len=None, seg_len_per_h
     return c
 
 
+def make_page_cache(k, v, table, k_scale=None, v_scale=None):
+    """Pages of keys and values [n_pages, H_kv, page, D] with the sequences' table [B, max_pages] int32: bf16, or uint8 codes
+    with the scales [n_pages, H_kv, page]; the tensors are kept alive with it."""
+    if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+        raise ValueError("k and v must be [n_pages, n_kv_heads, page, head_dim] and of one type")
+    if k.dtype != (torch.bfloat16 if k_scale is None else torch.uint8) or (k_scale is None) != (v_scale is None):
+        raise ValueError("pages are bfloat16 without scales, or uint8 codes with both scales")
+    for s in (k_scale, v_scale):
+        if s is not None and (s.dtype != torch.float32 or s.shape != k.shape[:3]):
+            raise ValueError("scales must be float32 [n_pages, n_kv_heads, page]")
+    if table.dim() != 2 or table.dtype != torch.int32:
+        raise ValueError("table must be int32 [batch, max_pages]")
+    c = pc_page_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(table), k.shape[0], k.shape[2], table.shape[1])
+    c.tensors = (k, v, table, k_scale, v_scale)
+    return c
+
+
+def _pages_fit(c, batch, n_kv_heads, head_dim):
+    k, _, table = c.tensors[:3]
+    if (k.shape[1], k.shape[3]) != (n_kv_heads, head_dim) or table.shape[0] != batch:
+        raise ValueError(f"pages of {tuple(k.shape)} with a table of {table.shape[0]} sequences are not those of {batch} "
+                         f"sequences, {n_kv_heads} KV heads of {head_dim}")
+
+
+def _strided(t, shape, dtype, name):
+    """The address of a tensor whose rows may lie apart, and its strides but the last (0 where there is one entry)."""
+    if not t.is_cuda or t.shape != shape or t.dtype != dtype or (t.stride(-1) != 1 and t.shape[-1] > 1):
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, is not {dtype} {tuple(shape)} on the GPU with "
+                         "consecutive values in a row")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is {torch.cuda.current_device()}")
+    if t.is_contiguous():
+        return t.data_ptr(), (0,) * (t.dim() - 1)
+    return t.data_ptr(), tuple(s if n > 1 else 0 for s, n in zip(t.stride()[:-1], t.shape))
+
+
+def _flat(t, n, dtype, name):
+    """The address of a tensor of n entries, or None."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n:
+        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} is not {n} entries of {dtype}")
+    return _ptr(t)
+
+
 def _rows_ref(c):
     return None if c is None else ctypes.byref(c)
 
@@ -452,6 +518,81 @@ def pc_verify_drafts(draft, draft_prob, target_prob, u, noise, batch, n_draft, v
     _check(lib().pc_verify_drafts(_ptr(draft), _ptr(draft_len), _ptr(draft_prob), _ptr(target_prob), _ptr(u), _ptr(noise),
                                   batch, n_draft, vocab, _ptr(tokens), _ptr(n_accepted), _ptr(len_in), _ptr(len_out),
                                   p, n, _stream()), "pc_verify_drafts")
+
+
+def pc_kv_append_paged(k_new, v_new, batch, n_new, n_kv_heads, head_dim, cache, len_in, len_out, pos=None, pos0=0, rope_base=0.0,
+                       parent=None, n_rows=None):
+    """cache: from make_page_cache.  k_new, v_new [B, n_new, H_kv, D], rows anywhere (the same strides for both)."""
+    _pages_fit(cache, batch, n_kv_heads, head_dim)
+    k = v = None
+    strides, i32 = (0, 0, 0), torch.int32
+    if n_new > 0 and batch > 0:
+        shape = (batch, n_new, n_kv_heads, head_dim)
+        (k, strides), (v, other) = _strided(k_new, shape, torch.bfloat16, "k_new"), _strided(v_new, shape, torch.bfloat16, "v_new")
+        if strides != other or not (any(strides) or k_new.is_contiguous()):
+            strides = tuple(s if m > 1 else 0 for s, m in zip(k_new.stride(), shape[:3]))
+            if strides != tuple(s if m > 1 else 0 for s, m in zip(v_new.stride(), shape[:3])) or not any(strides):
+                raise ValueError(f"k_new and v_new lie differently, or all rows at one place: strides {k_new.stride()}, {v_new.stride()}")
+    _check(lib().pc_kv_append_paged(k, v, *strides, _flat(parent, batch * n_new, i32, "parent"), _flat(n_rows, batch, i32, "n_rows"),
+                                    _flat(pos, batch, i32, "pos"), pos0, rope_base, batch, n_new, n_kv_heads, head_dim,
+                                    ctypes.byref(cache), _flat(len_in, batch, i32, "len_in"), _flat(len_out, batch, i32, "len_out"),
+                                    _stream()), "pc_kv_append_paged")
+
+
+def pc_tree_attn_workspace_bytes(cache, batch, n, n_q_heads, n_kv_heads, head_dim):
+    return int(lib().pc_tree_attn_workspace_bytes(ctypes.byref(cache), batch, n, n_q_heads, n_kv_heads, head_dim))
+
+
+def pc_tree_attn(q, cache, lens, batch, n, n_q_heads, n_kv_heads, head_dim, out, lse_out, ws, parent=None, n_rows=None, pos=None,
+                 pos0=0, rope_base=0.0, softmax_scale=0.0):
+    """cache: from make_page_cache.  q [B, n, H_q, D], a node's heads behind each other."""
+    _pages_fit(cache, batch, n_kv_heads, head_dim)
+    i32, rows = torch.int32, batch * n
+    at, strides = _strided(q, (batch, n, n_q_heads, head_dim), torch.bfloat16, "q")
+    if any(strides) and strides[2] not in (0, head_dim) or not (any(strides) or q.is_contiguous()) or \
+            (n_q_heads > 1 and any(strides) and strides[2] == 0):
+        raise ValueError(f"q: the heads of a node must lie behind each other, strides {q.stride()}")
+    if any(strides) and not any(strides[:2]):                               # one node of one sequence
+        strides = (0, 0, 0)
+    p, size = _ws(ws)
+    _check(lib().pc_tree_attn(at, *strides[:2], _flat(parent, rows, i32, "parent"), _flat(n_rows, batch, i32, "n_rows"),
+                              _flat(pos, batch, i32, "pos"), pos0, rope_base, softmax_scale, ctypes.byref(cache),
+                              _flat(lens, batch, i32, "lens"), batch, n, n_q_heads, n_kv_heads, head_dim,
+                              _flat(out, rows * n_q_heads * head_dim, torch.bfloat16, "out"),
+                              _flat(lse_out, rows * n_q_heads, torch.float32, "lse_out"), p, size, _stream()), "pc_tree_attn")
+
+
+def pc_token_logprobs_workspace_bytes(rows, vocab, n_top):
+    return int(lib().pc_token_logprobs_workspace_bytes(rows, vocab, n_top))
+
+
+def pc_token_logprobs(logits, rows, vocab, tokens, n_tokens, n_top, token_logprob, entropy, top_idx, top_logprob, ws):
+    """logits [rows, vocab] bfloat16 or float32, rows anywhere."""
+    if logits.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError(f"logits: {logits.dtype} is neither bfloat16 nor float32")
+    at, (stride,) = _strided(logits, (rows, vocab), logits.dtype, "logits")
+    if not logits.is_contiguous() and rows > 1 and stride < vocab:
+        raise ValueError(f"logits: rows overlap, strides {logits.stride()}")
+    i32, f32 = torch.int32, torch.float32
+    p, size = _ws(ws)
+    _check(lib().pc_token_logprobs(at, int(logits.dtype == f32), stride, _flat(tokens, rows * n_tokens, i32, "tokens"), n_tokens,
+                                   n_top, rows, vocab, _flat(token_logprob, rows * n_tokens, f32, "token_logprob"),
+                                   _flat(entropy, rows, f32, "entropy"), _flat(top_idx, rows * n_top, i32, "top_idx"),
+                                   _flat(top_logprob, rows * n_top, f32, "top_logprob"), p, size, _stream()), "pc_token_logprobs")
+
+
+def pc_tree_accept(tokens, parent, choice, batch, n, path, n_kept, next_token, choice_stride=1, cache=None, n_kv_heads=0, head_dim=0,
+                   len_in=None, len_out=None, pos=None, n_rows=None):
+    """cache: from make_page_cache, or None (nothing moves).  choice: a node every choice_stride entries."""
+    i32, rows = torch.int32, batch * n
+    if cache is not None:
+        _pages_fit(cache, batch, n_kv_heads, head_dim)
+    one = lambda t, name: _flat(t, batch, i32, name)
+    _check(lib().pc_tree_accept(_flat(tokens, rows, i32, "tokens"), _flat(parent, rows, i32, "parent"),
+                                _flat(choice, rows * choice_stride, i32, "choice"), choice_stride, one(n_rows, "n_rows"), batch, n,
+                                None if cache is None else ctypes.byref(cache), n_kv_heads, head_dim, one(len_in, "len_in"),
+                                one(len_out, "len_out"), one(pos, "pos"), _flat(path, rows, i32, "path"), one(n_kept, "n_kept"),
+                                one(next_token, "next_token"), _stream()), "pc_tree_accept")
 
 
 def pc_profile_begin(kernel=None):

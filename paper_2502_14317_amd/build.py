@@ -10,7 +10,7 @@ INCLUDE = os.path.join(os.path.dirname(PKG_DIR), "include")
 LIB_PATH = os.path.join(PKG_DIR, "libparallelcomp.so")
 SOURCES = ["pc_api.hip", "prep.hip", "gather.hip", "select.hip", "decode_attn.hip", "prefill_attn.hip",
            "scores.hip", "ceiling.hip", "self_info.hip", "decode_attn_fp8.hip", "serve_api.hip", "shared_attn.hip",
-           "row8.hip", "verify.hip"]
+           "row8.hip", "verify.hip", "paged_api.hip", "paged_append.hip", "tree_attn.hip", "logprobs.hip", "tree_accept.hip"]
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
                "-Wno-unused-command-line-argument",

@@ -234,10 +234,10 @@ struct SharedWalk {
       }
       const int left[1] = {cur.at.len - 32 * cur.at.blk};
       const bool masked = left[0] - most_unseen < 32;
-      const auto hidden = [&](int nc, int b, int i) { return i >= left[b] - unseen[nc]; };
+      const auto hidden = [&](int nc, int b, int bi, int j) { return 16 * bi + 4 * kk + j >= left[b] - unseen[nc]; };
       u32x4 p[NC][1];
       __builtin_amdgcn_s_setprio(0);
-      shared_softmax<NC, 1, VE, Q8>(s, sc, masked, hidden, kk, a.scale_log2, c.ref, c.sub, c.l, c.o, p);
+      shared_softmax<NC, 1, VE, Q8>(s, sc, masked, hidden, a.scale_log2, c.ref, c.sub, c.l, c.o, p);
       shared_values<NC, 1, VE, OWN>([&](int, int e) { return shared_value_operand<Q8>(vbuf, e); }, masked && most_unseen > 0, p, c.o);
       __builtin_amdgcn_sched_barrier(0);
       values(a, nx);
@@ -544,10 +544,10 @@ __device__ __forceinline__ void shared_row_tiles(const SharedArgs& a, int run, i
 #pragma unroll
     for (int b = 1; b < KB; ++b) least = min(least, left[b]);
     const bool masked = least - most_unseen < 32;
-    const auto hidden = [&](int nc, int b, int i) { return i >= left[b] - unseen[nc]; };
+    const auto hidden = [&](int nc, int b, int bi, int j) { return 16 * bi + 4 * kk + j >= left[b] - unseen[nc]; };
     u32x4 p[NC][KB];
     __builtin_amdgcn_s_setprio(0);
-    shared_softmax<NC, KB, VE, Q8>(s, sc, masked, hidden, kk, a.scale_log2, ref, sub, l_run, o, p);
+    shared_softmax<NC, KB, VE, Q8>(s, sc, masked, hidden, a.scale_log2, ref, sub, l_run, o, p);
     __builtin_amdgcn_s_setprio(1);
     shared_values<NC, KB, VE, OWN>([&](int b, int e) { return t.v[first + b][e][lane]; }, masked && most_unseen > 0, p, o);
     __builtin_amdgcn_s_setprio(0);

@@ -33,11 +33,12 @@ __device__ __forceinline__ u32x4 shared_value_operand(const Piece (&v)[8], int e
 // logit exceeds it, and then to the window above that logit: everything before is worth exp2(the move) of what it was.  So a
 // probability is never above 1, and sums of values times probabilities stay inside fp32 wherever those relative to the row's
 // maximum do.
-// hidden(nc, b, i): is key i of the lane's block b, 16 bi + 4 kk + j, out of column nc's sight; asked only where `masked`.
+// hidden(nc, b, bi, j): is key 16 bi + 4 kk + j of block b out of column nc's sight?  Asked only where `masked`, and without a
+// branch of its own: the compiler has lost the assignment behind one with several outcomes.
 struct SharedScales { floatx4 k[2], v[2]; };
 template <int NC, int KB, int VE, bool Q8, typename Hidden>
 __device__ __forceinline__ void shared_softmax(floatx4 (&s)[NC][KB][2], const SharedScales (&sc)[KB], bool masked, const Hidden& hidden,
-                                               int kk, float scale_log2, float (&ref)[NC], float (&sub)[NC],
+                                               float scale_log2, float (&ref)[NC], float (&sub)[NC],
                                                float (&l)[NC], floatx4 (&o)[NC][VE], u32x4 (&p)[NC][KB]) {
   if constexpr (Q8) {
 #pragma unroll
@@ -59,7 +60,7 @@ __device__ __forceinline__ void shared_softmax(floatx4 (&s)[NC][KB][2], const Sh
         for (int bi = 0; bi < 2; ++bi)
 #pragma unroll
           for (int j = 0; j < 4; ++j)
-            if (hidden(nc, b, 16 * bi + 4 * kk + j)) s[nc][b][bi][j] = -INFINITY;
+            if (hidden(nc, b, bi, j)) s[nc][b][bi][j] = -INFINITY;
   }
   float top[NC];
   bool beyond = false;

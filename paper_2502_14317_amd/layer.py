@@ -436,3 +436,177 @@ class SharedPrefixDecoder:
         B.pc_verify_drafts(draft, draft_prob, target_prob, u, noise, self.B, k, V, tokens, n_accepted, ws,
                            draft_len=draft_len, len_in=self.len, len_out=self.len)
         self._stand(k + 1)
+
+
+class PagedTreeDecoder:
+    """Answers of very unequal lengths out of one pool of pages, with trees of drafted tokens: a sequence's rows (its compressed
+    document, its query block, its answer) lie in pages of its own, taken as it grows and given back when it ends.
+
+      load(b, ...)    sequence b's document
+      step(q, k, v, parent)   the rows of every sequence's tree of this layer (its last token at the root, drafts below): appended,
+                      attended to; without a parent a chain, with one row an ordinary decoding step
+      accept(tokens, choice)  the path that the target's choices follow stays, its rows move together; the next token
+      release(b)      sequence b's pages are free again
+
+    Lengths and positions live on the device.  The host keeps a bound of each sequence's rows and reads the lengths only where a
+    sequence could pass the end of its pages; then it takes pages for it, and raises if there are none, before anything is
+    written.  A step in a captured graph takes no pages: reserve() them first, and see to it that the rows of the replays fit.
+    Rows behind a sequence's pages are dropped, and nobody sees them."""
+
+    def __init__(self, batch, n_pages, page, max_pages, n_q_heads, n_kv_heads, head_dim, rope_base, max_rows=1, softmax_scale=0.0,
+                 eight_bit=False, device="cuda"):
+        self.B, self.page, self.max_pages = batch, page, max_pages
+        self.Hq, self.Hkv, self.D = n_q_heads, n_kv_heads, head_dim
+        self.rope_base, self.scale, self.max_rows = rope_base, softmax_scale, max_rows
+        i32, shape = torch.int32, (n_pages, n_kv_heads, page)
+        kv = torch.uint8 if eight_bit else torch.bfloat16
+        self.k, self.v = (torch.zeros((*shape, head_dim), dtype=kv, device=device) for _ in "kv")
+        self.k_scale, self.v_scale = (torch.ones(shape, device=device) if eight_bit else None for _ in "kv")
+        self.table = torch.full((batch, max_pages), -1, dtype=i32, device=device)
+        self.len, self.len_new, self.pos = (torch.zeros((batch,), dtype=i32, device=device) for _ in range(3))
+        self.free = list(range(n_pages - 1, -1, -1))
+        self.pages = [None] * batch                                         # of a sequence; None: not loaded
+        self.most = [0] * batch                                             # no sequence has more rows that stand
+        self.known = True                                                   # False: graphs move the lengths unseen
+        self.at_hand = None                                                 # (rows, parent, n_rows) of the step that is not accepted yet
+        self.out = torch.empty((batch, max_rows, n_q_heads, head_dim), dtype=torch.bfloat16, device=device)
+        self.lse = torch.empty((batch, n_q_heads, max_rows), dtype=torch.float32, device=device)
+        self.path = torch.empty((batch, max_rows), dtype=i32, device=device)
+        self.n_kept, self.next_token = (torch.empty((batch,), dtype=i32, device=device) for _ in range(2))
+        self.cache = self.ws = None                                         # made with the first load
+
+    def _cache(self, table):
+        return B.make_page_cache(self.k, self.v, table, self.k_scale, self.v_scale)
+
+    def _ready(self, device):
+        if self.cache is not None:
+            return
+        if _capturing(self.len):
+            raise ValueError("load a document first")
+        self.cache = self._cache(self.table)
+        self.ws = B.alloc_workspace(max(B.pc_tree_attn_workspace_bytes(self.cache, self.B, m, self.Hq, self.Hkv, self.D)
+                                        for m in range(1, self.max_rows + 1)), device)
+
+    def reserve(self, b, rows):
+        """Pages for `rows` rows of sequence b."""
+        if _capturing(self.len):
+            raise ValueError("pages are taken outside of graphs")
+        have, need = self.pages[b] or [], (rows + self.page - 1) // self.page
+        more = need - len(have)
+        if more <= 0 and self.pages[b] is not None:
+            return
+        if need > self.max_pages:
+            raise ValueError(f"sequence {b}: {rows} rows are more than {self.max_pages} pages of {self.page}")
+        if more > len(self.free):
+            raise ValueError(f"sequence {b}: {more} pages more for {rows} rows, {len(self.free)} are free")
+        taken = [self.free.pop() for _ in range(max(more, 0))]
+        self.pages[b] = have + taken
+        if taken:
+            self.table[b, len(have):need].copy_(torch.tensor(taken, dtype=torch.int32))
+
+    def release(self, b):
+        """Sequence b has ended."""
+        if _capturing(self.len):
+            raise ValueError("a sequence ends outside of graphs")
+        if self.pages[b] is None:
+            return
+        self.free += reversed(self.pages[b])
+        self.pages[b], self.most[b] = None, 0
+        self.table[b].fill_(-1)
+        self.len[b], self.pos[b] = 0, 0
+
+    def load(self, b, kc, vc, pos, seg_len=None, k_tail=None, v_tail=None):
+        """kc, vc [n_seg, H_kv, k_t, D] bf16: the document's compacted segments (keys rotated), as the gather leaves them, of
+        seg_len[s] rows (None: k_t) each; k_tail, v_tail [n0, H_kv, D] rotated rows of the query block behind them, or None;
+        pos: the position of the sequence's next row.  What sequence b held before is released."""
+        n_seg, _, k_t, _ = kc.shape if kc.dim() == 4 else (0, 0, 0, 0)
+        if kc.shape != (n_seg, self.Hkv, k_t, self.D) or kc.shape != vc.shape or kc.dtype != torch.bfloat16 or vc.dtype != kc.dtype:
+            raise ValueError(f"kc {tuple(kc.shape)}, vc {tuple(vc.shape)}: not bfloat16 [n_seg, {self.Hkv}, k_t, {self.D}]")
+        lens = [k_t] * n_seg if seg_len is None else [int(x) for x in seg_len]
+        if len(lens) != n_seg or any(not 0 <= x <= k_t for x in lens):
+            raise ValueError(f"seg_len {lens} of {n_seg} segments of {k_t} rows")
+        if (k_tail is None) != (v_tail is None):
+            raise ValueError("k_tail and v_tail: both or neither")
+        n0 = 0 if k_tail is None else k_tail.shape[0]
+        if n0:
+            _must_be((n0, self.Hkv, self.D), torch.bfloat16, k_tail=k_tail, v_tail=v_tail)
+        if _capturing(self.len):
+            raise ValueError("a sequence is loaded outside of graphs")
+        total = sum(lens) + n0
+        self._fits(b, total)
+        self._ready(self.table.device)
+        self.release(b)
+        self.reserve(b, total)
+        i32, device = torch.int32, self.table.device
+        to = lambda x: torch.tensor(x, dtype=i32, device=device)
+        if n_seg and k_t:                                                   # each segment a sequence of its own, behind the one before
+            first = [sum(lens[:s]) for s in range(n_seg)]
+            B.pc_kv_append_paged(kc.transpose(1, 2), vc.transpose(1, 2), n_seg, k_t, self.Hkv, self.D,
+                                 self._cache(self.table[b].repeat(n_seg, 1)), to(first), None, n_rows=to(lens))
+        if n0:
+            B.pc_kv_append_paged(k_tail[None], v_tail[None], 1, n0, self.Hkv, self.D, self._cache(self.table[b:b + 1]), to([total - n0]), None)
+        self.len[b], self.pos[b] = total, pos
+        self.most[b] = total
+
+    def _fits(self, b, rows):
+        """Refuses a load that would not fit, before anything is released."""
+        need = (rows + self.page - 1) // self.page
+        if need > min(self.max_pages, len(self.free) + len(self.pages[b] or [])):
+            raise ValueError(f"sequence {b}: {rows} rows need {need} pages of {self.page}, {len(self.free)} are free, {self.max_pages} a "
+                             "sequence at most")
+
+    def _room(self, n):
+        """Pages for n rows more of every sequence."""
+        if _capturing(self.len):
+            self.known = False                                              # replays will move the lengths unseen
+            return
+        short = lambda: [b for b, p in enumerate(self.pages) if p is not None and self.most[b] + n > len(p) * self.page]
+        if not self.known or short():
+            self.most = self.len.tolist()
+        short = short()
+        need = [(self.most[b] + n + self.page - 1) // self.page for b in short]
+        if any(x > self.max_pages for x in need) or sum(need) - sum(len(self.pages[b]) for b in short) > len(self.free):
+            raise ValueError(f"{n} rows more do not fit: sequences {short} of {[self.most[b] for b in short]} rows, {len(self.free)} pages "
+                             f"of {self.page} are free, {self.max_pages} a sequence at most")
+        for b in short:
+            self.reserve(b, self.most[b] + n)
+
+    def step(self, q, k, v, parent=None, n_rows=None):
+        """q [B, n, H_q, D], k, v [B, n, H_kv, D] bf16 before RoPE, n <= max_rows: the nodes of every sequence's tree; parent
+        [B, n] int32 or None (a chain); n_rows [B] int32: how many are a sequence's (0: it does not take part), None: all, of
+        sequences that are all loaded.  Returns out [B, n, H_q, D] (a view of the step's buffer; other rows than n_rows of a sequence
+        are not written)."""
+        n = q.shape[1] if q.dim() == 4 else 0
+        if not 1 <= n <= self.max_rows or q.shape != (self.B, n, self.Hq, self.D) or k.shape != (self.B, n, self.Hkv, self.D) or \
+                v.shape != k.shape or any(t.dtype != torch.bfloat16 for t in (q, k, v)):
+            raise ValueError(f"q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}: not up to {self.max_rows} bfloat16 rows of this decoder")
+        for name, t, shape in (("parent", parent, (self.B, n)), ("n_rows", n_rows, (self.B,))):
+            if t is not None:
+                _must_be(shape, torch.int32, **{name: t})
+        if n_rows is None and None in self.pages:
+            raise ValueError(f"sequence {self.pages.index(None)} is not loaded: say with n_rows who takes part")
+        self._room(n)
+        self._ready(q.device)
+        B.pc_kv_append_paged(k, v, self.B, n, self.Hkv, self.D, self.cache, self.len, self.len_new, pos=self.pos,
+                             rope_base=self.rope_base, parent=parent, n_rows=n_rows)
+        out = self.out.view(-1)[:q.numel()].view(q.shape)
+        lse = self.lse.view(-1)[:self.B * self.Hq * n].view(self.B, self.Hq, n)
+        B.pc_tree_attn(q, self.cache, self.len_new, self.B, n, self.Hq, self.Hkv, self.D, out, lse, self.ws, parent=parent, n_rows=n_rows,
+                       pos=self.pos, rope_base=self.rope_base, softmax_scale=self.scale)
+        self.at_hand = (n, parent, n_rows)
+        return out
+
+    def accept(self, tokens, choice, choice_stride=1):
+        """pc_tree_accept of the step's trees: tokens [B, n], choice [B, n] (or [B, n, choice_stride], the first of each) int32.
+        Returns path [B, n], n_kept [B], next_token [B] (views of the decoder's buffers)."""
+        if self.at_hand is None:
+            raise ValueError("no step at hand")
+        n, parent, n_rows = self.at_hand
+        _must_be((self.B, n), torch.int32, tokens=tokens)
+        path = self.path.view(-1)[:self.B * n].view(self.B, n)
+        B.pc_tree_accept(tokens, parent, choice, self.B, n, path, self.n_kept, self.next_token, choice_stride=choice_stride,
+                         cache=self.cache, n_kv_heads=self.Hkv, head_dim=self.D, len_in=self.len_new, len_out=self.len, pos=self.pos,
+                         n_rows=n_rows)
+        self.at_hand = None
+        self.most = [m + n for m in self.most]
+        return path, self.n_kept, self.next_token
