@@ -136,55 +136,66 @@ struct TreeWalk {
     keys(a, cur);
     values(a, cur);
   }
-  // above: the nodes that the lane's columns see, as bits
-  __device__ __forceinline__ void run(const TreeArgs& a, const TreePiece& x, SharedColumns<D, NC>& c, const unsigned long long (&above)[NC], float (*scale)[32]) {
+  // One block.  MASKED: some of its keys are not there, or rows of the tree; few blocks are, so that the query operands come from
+  // LDS there and leave their registers to the masks (in registers throughout, 128 values a row and 32 columns, 89 to 126
+  // registers spilled, and every block waited for its own: 16 sequences of 11000 rows, 64 query rows a KV head, 363 us)
+  template <bool MASKED>
+  __device__ __forceinline__ void step(const TreeArgs& a, const TreePiece& x, SharedColumns<D, NC>& c, const unsigned long long (&above)[NC], float (*scale)[32],
+                                       const uint16_t (*hi)[D + 8], const uint16_t (*lo)[D + 8], int col0) {
     const int lane = threadIdx.x % PC_WAVE, kk = lane / 16;
-    while (cur.blk < end) {
-      const TreeBlock nx = block(a, x, cur.blk + 1);
-      if constexpr (Q8) scale[lane / 32][lane % 32] = sbuf;
-      floatx4 s[NC][1][2];
+    const TreeBlock nx = block(a, x, cur.blk + 1);
+    if constexpr (Q8) scale[lane / 32][lane % 32] = sbuf;
+    floatx4 s[NC][1][2];
 #pragma unroll
-      for (int nc = 0; nc < NC; ++nc)
+    for (int nc = 0; nc < NC; ++nc)
 #pragma unroll
-        for (int bi = 0; bi < 2; ++bi) s[nc][0][bi] = floatx4{0.f, 0.f, 0.f, 0.f};
+      for (int bi = 0; bi < 2; ++bi) s[nc][0][bi] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ks = 0; ks < KSTEPS; ++ks)
+    for (int ks = 0; ks < KSTEPS; ++ks)
 #pragma unroll
-        for (int bi = 0; bi < 2; ++bi) {
-          u32x4 ka;
+      for (int bi = 0; bi < 2; ++bi) {
+        u32x4 ka;
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            if constexpr (Q8) ka[w] = shared_widen(kbuf[bi][ks / 2][2 * (ks % 2) + w / 2], w % 2);
-            else ka[w] = kbuf[bi][ks][w];
+        for (int w = 0; w < 4; ++w) {
+          if constexpr (Q8) ka[w] = shared_widen(kbuf[bi][ks / 2][2 * (ks % 2) + w / 2], w % 2);
+          else ka[w] = kbuf[bi][ks][w];
+        }
+#pragma unroll
+        for (int h = 1; h >= 0; --h)
+#pragma unroll
+          for (int nc = 0; nc < NC; ++nc) {
+            bf16x8 q;
+            if constexpr (MASKED) q = *(const bf16x8*)&(h ? lo : hi)[col0 + 16 * nc + lane % 16][shared_query_at(Q8, ks, kk)];
+            else q = c.q[h][nc][ks];
+            s[nc][0][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(bf16x8*)&ka, q, s[nc][0][bi], 0, 0, 0);
           }
-#pragma unroll
-          for (int h = 1; h >= 0; --h)
-#pragma unroll
-            for (int nc = 0; nc < NC; ++nc)
-              s[nc][0][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(bf16x8*)&ka, c.q[h][nc][ks], s[nc][0][bi], 0, 0, 0);
-        }
-      __builtin_amdgcn_sched_barrier(0);
-      keys(a, nx);
-      SharedScales sc[1];
-      if constexpr (Q8) {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int bi = 0; bi < 2; ++bi) {
-          sc[0].k[bi] = *(const floatx4*)&scale[0][16 * bi + 4 * kk];
-          sc[0].v[bi] = *(const floatx4*)&scale[1][16 * bi + 4 * kk];
-        }
       }
-      const int rel = 32 * cur.blk - x.base;                 // the block's first key as a node of the tree
-      const bool tree = rel + 32 > 0, masked = tree || cur.keys[0] < 16 || cur.keys[1] < 16;
-      const auto hidden = [&](int nc, int, int bi, int j) { return !(tree_sight(above[nc], rel + 16 * bi + 4 * kk, cur.keys[bi] - 4 * kk) >> j & 1); };
-      u32x4 p[NC][1];
-      shared_softmax<NC, 1, VE, Q8>(s, sc, masked, hidden, a.scale_log2, c.ref, c.sub, c.l, c.o, p);
-      shared_values<NC, 1, VE, true>([&](int, int e) { return shared_value_operand<Q8>(vbuf, e); }, tree, p, c.o);
-      __builtin_amdgcn_sched_barrier(0);
-      values(a, nx);
-      cur = nx;
+    __builtin_amdgcn_sched_barrier(0);
+    keys(a, nx);
+    SharedScales sc[1];
+    if constexpr (Q8) {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int bi = 0; bi < 2; ++bi) {
+        sc[0].k[bi] = *(const floatx4*)&scale[0][16 * bi + 4 * kk];
+        sc[0].v[bi] = *(const floatx4*)&scale[1][16 * bi + 4 * kk];
+      }
     }
+    const int rel = 32 * cur.blk - x.base;                   // the block's first key as a node of the tree
+    const auto hidden = [&](int nc, int, int bi, int j) { return !(tree_sight(above[nc], rel + 16 * bi + 4 * kk, cur.keys[bi] - 4 * kk) >> j & 1); };
+    u32x4 p[NC][1];
+    shared_softmax<NC, 1, VE, Q8>(s, sc, MASKED, hidden, a.scale_log2, c.ref, c.sub, c.l, c.o, p);
+    shared_values<NC, 1, VE, MASKED>([&](int, int e) { return shared_value_operand<Q8>(vbuf, e); }, rel + 32 > 0, p, c.o);
+    __builtin_amdgcn_sched_barrier(0);
+    values(a, nx);
+    cur = nx;
+  }
+  // above: the nodes that the lane's columns see, as bits.  The blocks that every column sees whole come first.
+  __device__ __forceinline__ void run(const TreeArgs& a, const TreePiece& x, SharedColumns<D, NC>& c, const unsigned long long (&above)[NC], float (*scale)[32],
+                                      const uint16_t (*hi)[D + 8], const uint16_t (*lo)[D + 8], int col0) {
+    while (cur.keys[0] == 16 && cur.keys[1] == 16 && 32 * cur.blk + 32 <= x.base) step<false>(a, x, c, above, scale, hi, lo, col0);
+    while (cur.blk < end) step<true>(a, x, c, above, scale, hi, lo, col0);
   }
 };
 
@@ -267,8 +278,8 @@ __device__ __forceinline__ void tree_piece(const TreeArgs& a, const TreePiece& x
   unsigned long long above[NC];
 #pragma unroll
   for (int nc = 0; nc < NC; ++nc) above[nc] = sm.above[pc_div(x.row0 + min(col0 + 16 * nc + lane % 16, x.n_here - 1), a.group_div)];
-  __syncthreads();
-  walk.run(a, x, c, above, sm.few.scale[wave]);
+  walk.run(a, x, c, above, sm.few.scale[wave], sm.few.q[0], sm.few.q[1], col0);
+  __syncthreads();                                           // (the query rows are written over)
   shared_columns_out<D, NC>(c, sm.few, wk, col0, x.n_here);
   __syncthreads();
   for (int idx = threadIdx.x; idx < x.n_here * (D / 4); idx += TREE_THREADS) {
