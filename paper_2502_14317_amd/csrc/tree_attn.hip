@@ -10,12 +10,24 @@
 // tile of query rows: so a batch of very unequal lengths keeps every CU busy, whatever the table's width.  A share is a
 // piece of one sequence or of several; each piece leaves a partial (o, lse) a row at place share + sequence (both
 // only grow along the keys, so a place is taken once), and tree_join_kernel joins a sequence's.
+#include <type_traits>
+#include "decode_core.h"
 #include "paged.h"
 #include "shared_core.h"
 #include "serve.h"
 
 #define TREE_WAVES 4
 #define TREE_THREADS (TREE_WAVES * PC_WAVE)
+// the N newest loads of this wavefront may still be on their way
+#define TREE_WAIT_LOADS(N) __builtin_amdgcn_s_waitcnt(0x0F70 | ((N) & 15) | (((N) >> 4) << 14))
+// ... and a barrier, with LDS reads done.  (A fence would wait for every load that goes to LDS.)
+#define TREE_TILE_BARRIER(N)                                                         \
+  do {                                                                               \
+    asm volatile("" ::: "memory");                                                   \
+    __builtin_amdgcn_s_waitcnt(0x0070 | ((N) & 15) | (((N) >> 4) << 14));            \
+    __builtin_amdgcn_s_barrier();                                                    \
+    asm volatile("" ::: "memory");                                                   \
+  } while (0)
 
 struct TreeArgs {
   PcTreeCall c;
@@ -27,6 +39,13 @@ struct TreeArgs {
   float* part_lse;         // [n_shares + B][H_kv][n group]
   int2* span;              // [B] first and last share of a sequence
 };
+
+// The lane's number again, as a value of its own: what is computed from it is computed here, and not kept in registers from in front
+// of a loop on
+__device__ __forceinline__ int tree_own(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
 
 // 32-key blocks that sequence b has: none where it has no nodes
 __device__ __forceinline__ int tree_len(const PcTreeCall& c, int b) {
@@ -58,7 +77,30 @@ struct TreeBlock {
   int keys[2];             // that are there
 };
 
-template <int D, int NC, int WK, bool Q8>
+// A wavefront's window of the table: 64 entries from `first` on, and the 64 behind them, which are on their way
+struct TreeTable {
+  int here, next, first;
+  __device__ __forceinline__ int entries(const TreeArgs& a, const TreePiece& x, int at) const {
+    const int i = min(at + (int)(threadIdx.x % PC_WAVE), a.c.pages.max_pages - 1);
+    return a.c.pages.table[(long long)x.b * a.c.pages.max_pages + i];
+  }
+  __device__ __forceinline__ void begin(const TreeArgs& a, const TreePiece& x, int at) {
+    first = at;
+    here = entries(a, x, at);
+    next = entries(a, x, at + PC_WAVE);
+  }
+  // the row of the pool where key `key` lies, -1 if it is not there; keys are asked for in order
+  __device__ __forceinline__ long long row(const TreeArgs& a, const TreePiece& x, int key) {
+    const int at = key >> a.c.pages.shift;
+    if (at >= first + PC_WAVE) {
+      here = next; first += PC_WAVE;
+      next = entries(a, x, first + PC_WAVE);
+    }
+    return pc_pool_row(a.c.pages, __builtin_amdgcn_readlane(here, at - first), key, x.g, a.c.n_kv_heads);
+  }
+};
+
+template <int D, int NC, bool Q8>
 struct TreeWalk {
   static constexpr int KSTEPS = D / 32, VE = D / 16, ELEM = Q8 ? 1 : 2, ROW = D * ELEM;
   static constexpr int KP = Q8 ? D / 64 : KSTEPS;
@@ -68,30 +110,17 @@ struct TreeWalk {
   float sbuf;
   TreeBlock cur;
   int end;                                                   // the run's last block is in front of it
-  int tab, tab_next, tab0;                                   // 64 entries of the table from tab0 on, and the 64 behind them
+  TreeTable tab;
 
-  __device__ __forceinline__ int entries(const TreeArgs& a, const TreePiece& x, int at) const {
-    const int i = min(at + (int)(threadIdx.x % PC_WAVE), a.c.pages.max_pages - 1);
-    return a.c.pages.table[(long long)x.b * a.c.pages.max_pages + i];
-  }
   __device__ __forceinline__ TreeBlock block(const TreeArgs& a, const TreePiece& x, int blk) {
     TreeBlock t;
     t.blk = blk;
-    const int shift = a.c.pages.shift;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      t.row[h] = 0; t.keys[h] = 0;
       const int key = 32 * blk + 16 * h;
-      if (blk >= end || key >= x.len) continue;
-      const int at = key >> shift;
-      if (at >= tab0 + PC_WAVE) {                            // (entries are taken in order)
-        tab = tab_next; tab0 += PC_WAVE;
-        tab_next = entries(a, x, tab0 + PC_WAVE);
-      }
-      const long long row = pc_pool_row(a.c.pages, __builtin_amdgcn_readlane(tab, at - tab0), key, x.g, a.c.n_kv_heads);
-      if (row < 0) continue;
-      t.row[h] = row;
-      t.keys[h] = min(16, x.len - key);
+      t.row[h] = blk < end && key < x.len ? tab.row(a, x, key) : -1;
+      t.keys[h] = t.row[h] < 0 ? 0 : min(16, x.len - key);
+      t.row[h] = max(t.row[h], 0LL);
     }
     return t;
   }
@@ -106,7 +135,7 @@ struct TreeWalk {
     for (int h = 0; h < 2; ++h) {
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)a.c.pages.k + t.row[h] * ROW), 0, t.keys[h] * ROW, 0x00020000);
 #pragma unroll
-      for (int p = 0; p < KP; ++p) kbuf[h][p] = __builtin_amdgcn_raw_buffer_load_b128(r, c16 * ROW + 16 * kk, 64 * p, 0);
+      for (int p = 0; p < KP; ++p) kbuf[h][p] = __builtin_amdgcn_raw_buffer_load_b128(r, c16 * ROW + 16 * kk, 64 * p, PC_BUF_NT);
     }
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -118,20 +147,18 @@ struct TreeWalk {
       const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)a.c.pages.v + t.row[h] * ROW), 0, t.keys[h] * ROW, 0x00020000);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if constexpr (sizeof(vpiece) == 16) vbuf[4 * h + i] = __builtin_amdgcn_raw_buffer_load_b128(r, off, i * ROW, 0);
-        else if constexpr (sizeof(vpiece) == 8) vbuf[4 * h + i] = __builtin_amdgcn_raw_buffer_load_b64(r, off, i * ROW, 0);
-        else vbuf[4 * h + i] = __builtin_amdgcn_raw_buffer_load_b32(r, off, i * ROW, 0);
+        if constexpr (sizeof(vpiece) == 16) vbuf[4 * h + i] = __builtin_amdgcn_raw_buffer_load_b128(r, off, i * ROW, PC_BUF_NT);
+        else if constexpr (sizeof(vpiece) == 8) vbuf[4 * h + i] = __builtin_amdgcn_raw_buffer_load_b64(r, off, i * ROW, PC_BUF_NT);
+        else vbuf[4 * h + i] = __builtin_amdgcn_raw_buffer_load_b32(r, off, i * ROW, PC_BUF_NT);
       }
     }
     __builtin_amdgcn_sched_barrier(0);
   }
-  // the wk-th of the piece's WK runs of blocks
-  __device__ __forceinline__ void begin(const TreeArgs& a, const TreePiece& x, int blk0, int n_blk, int wk) {
-    const int first = blk0 + (int)((long long)n_blk * wk / WK);
-    end = blk0 + (int)((long long)n_blk * (wk + 1) / WK);
-    tab0 = (32 * first) >> a.c.pages.shift;
-    tab = entries(a, x, tab0);
-    tab_next = entries(a, x, tab0 + PC_WAVE);
+  // the wavefront's run of the piece's blocks
+  __device__ __forceinline__ void begin(const TreeArgs& a, const TreePiece& x, int blk0, int n_blk, int wave) {
+    const int first = blk0 + (int)((long long)n_blk * wave / TREE_WAVES);
+    end = blk0 + (int)((long long)n_blk * (wave + 1) / TREE_WAVES);
+    tab.begin(a, x, (32 * first) >> a.c.pages.shift);
     cur = block(a, x, first);
     keys(a, cur);
     values(a, cur);
@@ -141,7 +168,7 @@ struct TreeWalk {
   // registers spilled, and every block waited for its own: 16 sequences of 11000 rows, 64 query rows a KV head, 363 us)
   template <bool MASKED>
   __device__ __forceinline__ void step(const TreeArgs& a, const TreePiece& x, SharedColumns<D, NC>& c, const unsigned long long (&above)[NC], float (*scale)[32],
-                                       const uint16_t (*hi)[D + 8], const uint16_t (*lo)[D + 8], int col0) {
+                                       const uint16_t (*hi)[D + 8], const uint16_t (*lo)[D + 8]) {
     const int lane = threadIdx.x % PC_WAVE, kk = lane / 16;
     const TreeBlock nx = block(a, x, cur.blk + 1);
     if constexpr (Q8) scale[lane / 32][lane % 32] = sbuf;
@@ -165,7 +192,7 @@ struct TreeWalk {
 #pragma unroll
           for (int nc = 0; nc < NC; ++nc) {
             bf16x8 q;
-            if constexpr (MASKED) q = *(const bf16x8*)&(h ? lo : hi)[col0 + 16 * nc + lane % 16][shared_query_at(Q8, ks, kk)];
+            if constexpr (MASKED) q = *(const bf16x8*)&(h ? lo : hi)[16 * nc + lane % 16][shared_query_at(Q8, ks, kk)];
             else q = c.q[h][nc][ks];
             s[nc][0][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(bf16x8*)&ka, q, s[nc][0][bi], 0, 0, 0);
           }
@@ -193,34 +220,59 @@ struct TreeWalk {
   }
   // above: the nodes that the lane's columns see, as bits.  The blocks that every column sees whole come first.
   __device__ __forceinline__ void run(const TreeArgs& a, const TreePiece& x, SharedColumns<D, NC>& c, const unsigned long long (&above)[NC], float (*scale)[32],
-                                      const uint16_t (*hi)[D + 8], const uint16_t (*lo)[D + 8], int col0) {
-    while (cur.keys[0] == 16 && cur.keys[1] == 16 && 32 * cur.blk + 32 <= x.base) step<false>(a, x, c, above, scale, hi, lo, col0);
-    while (cur.blk < end) step<true>(a, x, c, above, scale, hi, lo, col0);
+                                      const uint16_t (*hi)[D + 8], const uint16_t (*lo)[D + 8]) {
+    while (cur.keys[0] == 16 && cur.keys[1] == 16 && 32 * cur.blk + 32 <= x.base) step<false>(a, x, c, above, scale, hi, lo);
+    while (cur.blk < end) step<true>(a, x, c, above, scale, hi, lo);
   }
 };
 
-template <int D, int NC, int WR>
+struct TreeScanLds { int sums[TREE_WAVES], begin[2]; };      // of the lengths' scan
+template <int D, int NC>
 struct TreeLds {
-  SharedFewLds<D, NC, WR, TREE_WAVES> few;
-  unsigned long long above[PC_TREE_NODES];
-  int sums[TREE_WAVES];    // of the lengths' scan
-  int begin[2];
+  SharedFewLds<D, NC, 1, TREE_WAVES> few;
+  TreeScanLds scan;
 };
+// The nodes that node t sees, from the lanes' own
+__device__ __forceinline__ unsigned long long tree_above_of(unsigned long long mine, int t) {
+  const uint32_t lo = (uint32_t)__shfl((int)(uint32_t)mine, t), hi = (uint32_t)__shfl((int)(uint32_t)(mine >> 32), t);
+  return (unsigned long long)hi << 32 | lo;
+}
+// Four pairs of a row turned by their angles, into two bf16 parts of each half
+__device__ __forceinline__ void tree_turn(u32x4& u, u32x4& v, u32x4& ul, u32x4& vl, double at, const double (&theta)[8]) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    float y1[2], y2[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const float x1 = b ? bf16_hi_to_f32(u[w]) : bf16_lo_to_f32(u[w]), x2 = b ? bf16_hi_to_f32(v[w]) : bf16_lo_to_f32(v[w]);
+      float sn, cs;
+      pc_sincos_f32(at * theta[2 * w + b], sn, cs);
+      y1[b] = x1 * cs - x2 * sn; y2[b] = x2 * cs + x1 * sn;
+    }
+    uint32_t hi, lo;
+    split_bf16x2(y1[0], y1[1], hi, lo);
+    u[w] = hi; ul[w] = lo;
+    split_bf16x2(y2[0], y2[1], hi, lo);
+    v[w] = hi; vl[w] = lo;
+  }
+}
 
 // Query rows -> LDS as two bf16 parts, rotated at their nodes' positions (rows behind the last one: zeros).  D / 16 threads a
-// row, 8 values of each half.
+// row, 8 values of each half.  mine: what the lane's node sees
 template <int D, int N>
-__device__ __forceinline__ void tree_query_rows(const TreeArgs& a, const TreePiece& x, const unsigned long long* above, uint16_t (*hi)[D + 8],
+__device__ __forceinline__ void tree_query_rows(const TreeArgs& a, const TreePiece& x, unsigned long long mine, uint16_t (*hi)[D + 8],
                                                 uint16_t (*lo)[D + 8]) {
   constexpr int HALF = D / 2, TPR = HALF / 8, PASS = TREE_THREADS / TPR, PASSES = (N + PASS - 1) / PASS;
-  const int i0 = threadIdx.x % TPR * 8;
+  const int thread = tree_own(threadIdx.x), i0 = thread % TPR * 8;
   u32x4 lo_half[PASSES], hi_half[PASSES];
+  int depth[PASSES];
 #pragma unroll
   for (int n = 0; n < PASSES; ++n) {
-    const int r = x.row0 + min((int)threadIdx.x / TPR + n * PASS, x.n_here - 1);
+    const int r = x.row0 + min(thread / TPR + n * PASS, x.n_here - 1);
     const int t = pc_div(r, a.group_div), h = r - t * a.group;
     const uint16_t* src = a.c.q + x.b * a.c.batch_stride + t * a.c.row_stride + (x.g * a.group + h) * D + i0;
     lo_half[n] = *(const u32x4*)src; hi_half[n] = *(const u32x4*)(src + HALF);
+    depth[n] = __popcll(tree_above_of(mine, t)) - 1;
   }
   double theta[8];
   double first = 0.0;
@@ -231,72 +283,341 @@ __device__ __forceinline__ void tree_query_rows(const TreeArgs& a, const TreePie
   }
 #pragma unroll
   for (int n = 0; n < PASSES; ++n) {
-    const int r = threadIdx.x / TPR + n * PASS;
+    const int r = thread / TPR + n * PASS;
     if (r >= N) break;
     u32x4 u = lo_half[n], v = hi_half[n], ul = {0, 0, 0, 0}, vl = {0, 0, 0, 0};
     if (r >= x.n_here) u = v = u32x4{0, 0, 0, 0};
-    if (a.c.pos) {
-      const int t = pc_div(x.row0 + min(r, x.n_here - 1), a.group_div);
-      const double at = first + (__popcll(above[t]) - 1);
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        float y1[2], y2[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const float x1 = b ? bf16_hi_to_f32(u[w]) : bf16_lo_to_f32(u[w]), x2 = b ? bf16_hi_to_f32(v[w]) : bf16_lo_to_f32(v[w]);
-          float sn, cs;
-          pc_sincos_f32(at * theta[2 * w + b], sn, cs);
-          y1[b] = x1 * cs - x2 * sn; y2[b] = x2 * cs + x1 * sn;
-        }
-        u[w] = pack_bf16x2(y1[0], y1[1]); v[w] = pack_bf16x2(y2[0], y2[1]);
-        ul[w] = pack_bf16x2(y1[0] - bf16_lo_to_f32(u[w]), y1[1] - bf16_hi_to_f32(u[w]));
-        vl[w] = pack_bf16x2(y2[0] - bf16_lo_to_f32(v[w]), y2[1] - bf16_hi_to_f32(v[w]));
-      }
-    }
+    if (a.c.pos) tree_turn(u, v, ul, vl, first + depth[n], theta);
     *(u32x4*)&hi[r][i0] = u; *(u32x4*)&hi[r][i0 + HALF] = v;
     *(u32x4*)&lo[r][i0] = ul; *(u32x4*)&lo[r][i0 + HALF] = vl;
   }
 }
 
-// Blocks blk0 .. of a sequence for its query rows -> a partial at `place`
-template <int D, int NC, int WR, bool Q8>
-__device__ __forceinline__ void tree_piece(const TreeArgs& a, const TreePiece& x, int blk0, int n_blk, int place, TreeLds<D, NC, WR>& sm) {
-  constexpr int WK = TREE_WAVES / WR;
-  const int lane = threadIdx.x % PC_WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PC_WAVE);
-  const int wk = wave / WR, col0 = 16 * NC * (wave % WR);
+__device__ __forceinline__ long long tree_part_row(const TreeArgs& a, const TreePiece& x, int place, int r) {
+  return ((long long)place * a.c.n_kv_heads + x.g) * (a.c.n * a.group) + x.row0 + r;
+}
+
+// Blocks blk0 .. of a sequence for its 16 NC query rows -> a partial at `place`; a wavefront has a part of the blocks
+template <int D, int NC, bool Q8>
+__device__ __forceinline__ void tree_piece(const TreeArgs& a, const TreePiece& x, int blk0, int n_blk, int place, TreeLds<D, NC>& sm) {
+  const int lane = tree_own(threadIdx.x % PC_WAVE), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PC_WAVE);
   const unsigned long long mine = pc_tree_above(a.c.parent, x.b, a.c.n, lane);
-  __syncthreads();                                           // (the piece before this one is done with LDS)
-  if (wave == 0) sm.above[lane] = mine;
-  __syncthreads();
-  TreeWalk<D, NC, WK, Q8> walk;
-  walk.begin(a, x, blk0, n_blk, wk);
-  tree_query_rows<D, 16 * NC * WR>(a, x, sm.above, sm.few.q[0], sm.few.q[1]);
-  __syncthreads();
+  TreeWalk<D, NC, Q8> walk;
+  walk.begin(a, x, blk0, n_blk, wave);
+  PC_LDS_BARRIER();                                          // (the piece before this one is done with LDS)
+  tree_query_rows<D, 16 * NC>(a, x, mine, sm.few.q[0], sm.few.q[1]);
+  PC_LDS_BARRIER();
   SharedColumns<D, NC> c;
   c.clear();
-  shared_query_operands<D, NC, Q8>(c, sm.few.q[0], sm.few.q[1], col0);
+  shared_query_operands<D, NC, Q8>(c, sm.few.q[0], sm.few.q[1], 0);
   unsigned long long above[NC];
 #pragma unroll
-  for (int nc = 0; nc < NC; ++nc) above[nc] = sm.above[pc_div(x.row0 + min(col0 + 16 * nc + lane % 16, x.n_here - 1), a.group_div)];
-  walk.run(a, x, c, above, sm.few.scale[wave], sm.few.q[0], sm.few.q[1], col0);
-  __syncthreads();                                           // (the query rows are written over)
-  shared_columns_out<D, NC>(c, sm.few, wk, col0, x.n_here);
-  __syncthreads();
+  for (int nc = 0; nc < NC; ++nc) above[nc] = tree_above_of(mine, pc_div(x.row0 + min(16 * nc + lane % 16, x.n_here - 1), a.group_div));
+  walk.run(a, x, c, above, sm.few.scale[wave], sm.few.q[0], sm.few.q[1]);
+  PC_LDS_BARRIER();                                          // (the query rows are written over)
+  shared_columns_out<D, NC>(c, sm.few, wave, 0, x.n_here);
+  PC_LDS_BARRIER();
   for (int idx = threadIdx.x; idx < x.n_here * (D / 4); idx += TREE_THREADS) {
     const int r = idx / (D / 4), d4 = idx % (D / 4) * 4;
     SharedRowSum sum;
     sum.clear();
 #pragma unroll
-    for (int w = 0; w < WK; ++w) sum.add(sm.few.m[w][r], sm.few.l[w][r], *(const floatx4*)&sm.few.o[w][r][d4]);
-    const long long row = ((long long)place * a.c.n_kv_heads + x.g) * (a.c.n * a.group) + x.row0 + r;
+    for (int w = 0; w < TREE_WAVES; ++w) sum.add(sm.few.m[w][r], sm.few.l[w][r], *(const floatx4*)&sm.few.o[w][r][d4]);
+    const long long row = tree_part_row(a, x, place, r);
     *(floatx4*)(a.part_o + row * D + d4) = sum.mean();
     if (d4 == 0) a.part_lse[row] = sum.lse();
   }
 }
 
+// ------------------------------------------------------------------------------------------ many rows
+// Blocks of 32 keys on their way from memory straight into LDS, some 64 KB of them, each read there by all four wavefronts, which
+// have 16 NC query rows each.  A row is PPR pieces of 16 bytes, piece p of row r in place p ^ swizzle(r): so the
+// matrix operands (16 rows at once, or four whole ones) come without bank conflicts, and a load instruction brings whole rows.
+// (Keys straight into registers, two wavefronts to a key, keep half as many bytes on their way: 16 sequences of 11000 rows, 64
+// query rows a KV head, 188 us.)
+template <int D, bool Q8>
+struct TreeTiles {
+  static constexpr int RB = D * (Q8 ? 1 : 2), PPR = RB / 16;        // bytes, pieces of a row
+  static constexpr int STAGES = RB == 256 ? 4 : 8;
+  static constexpr int LOADS = RB / 64 + (Q8 ? 1 : 0);              // of a wavefront, a block
+  struct Lds {
+    uint8_t rows[STAGES][2][32 * RB];                               // [keys, values]
+    float scale[STAGES][2][32];
+    unsigned long long above[PC_TREE_NODES];
+    TreeScanLds scan;
+  };
+  __device__ __forceinline__ static int swizzle(int row) { return PPR == 4 ? row >> 1 & 3 : row & (PPR - 1); }
+};
+
+template <int D, int NC, bool Q8>
+__device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePiece& x, int blk0, int n_blk, int place,
+                                                typename TreeTiles<D, Q8>::Lds& sm) {
+  typedef TreeTiles<D, Q8> Tiles;
+  constexpr int KSTEPS = D / 32, VE = D / 16, RB = Tiles::RB, PPR = Tiles::PPR, STAGES = Tiles::STAGES, AHEAD = STAGES - 1;
+  typedef uint32_t vpiece __attribute__((ext_vector_type(VE * (Q8 ? 1 : 2) / 4)));
+  typedef __attribute__((address_space(3))) void* lptr_t;
+  const int lane = tree_own(threadIdx.x % PC_WAVE), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PC_WAVE);
+  const int kk = lane / 16, c16 = lane % 16;
+  const unsigned long long mine = pc_tree_above(a.c.parent, x.b, a.c.n, lane);
+  const int end = blk0 + n_blk;
+
+  TreeTable tab;
+  tab.begin(a, x, (32 * blk0) >> a.c.pages.shift);
+
+  // ---- the wavefront's query rows, as they lie in the operands: both values of a pair are the same lane's
+  SharedColumns<D, NC> c;
+  c.clear();
+  auto node_of = [&](int nc, int c16) { return pc_div(x.row0 + min(16 * (NC * wave + nc) + c16, x.n_here - 1), a.group_div); };
+  u32x4 q[NC][KSTEPS];
+#pragma unroll
+  for (int nc = 0; nc < NC; ++nc) {
+    const int r = x.row0 + min(16 * (NC * wave + nc) + c16, x.n_here - 1), t = node_of(nc, c16);
+    const uint16_t* src = a.c.q + x.b * a.c.batch_stride + t * a.c.row_stride + (x.g * a.group + r - t * a.group) * D + 8 * kk;
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) q[nc][ks] = *(const u32x4*)(src + 32 * ks);
+  }
+  // Waited for in front of the loads to LDS: behind those the compiler, which does not count them through the loop, waits for too many
+  asm volatile("" : "+v"(tab.here), "+v"(tab.next));
+#pragma unroll
+  for (int nc = 0; nc < NC; ++nc)
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks) asm volatile("" : "+v"(q[nc][ks]));
+
+  // ---- the blocks' loads.  Rows of 128 bytes or more: wavefront w brings rows 8 w .. of keys and values; shorter ones: half w % 2 of
+  // the keys (w < 2) or values.  Rows that are not there are out of the descriptor: zeros.
+  const int my_half = RB >= 128 ? wave / 2 : wave % 2, row0 = RB >= 128 ? 8 * wave : 16 * (wave % 2);      // (of the block)
+  const int at_row = row0 % 16 + lane / PPR;                         // of the half
+  const int off = at_row * RB + 16 * (lane % PPR ^ Tiles::swizzle(at_row));
+  uint32_t there = 0;                                                // two bits a block: are the halves' pages there
+  auto issue = [&](int blk) __attribute__((always_inline)) {
+    long long row[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int key = 32 * blk + 16 * h;
+      row[h] = blk < end && key < x.len ? tab.row(a, x, key) : -1;
+    }
+    there = there << 2 | (row[0] >= 0 ? 1u : 0u) | (row[1] >= 0 ? 2u : 0u);
+    const int stage = (blk - blk0) & (STAGES - 1);
+    const long long r = my_half ? row[1] : row[0];
+    const int keys = r < 0 ? 0 : min(16, x.len - 32 * blk - 16 * my_half);
+    const long long at = r < 0 ? 0 : r;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      if (RB < 128 && kv != wave / 2) continue;
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)(kv ? a.c.pages.v : a.c.pages.k) + at * RB), 0, keys * RB, 0x00020000);
+#pragma unroll
+      for (int i = 0; i < (RB == 256 ? 2 : 1); ++i)                  // (rows 4 further on: another bit of the swizzle)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(sm.rows[stage][kv] + (row0 + 4 * i) * RB), 16, off ^ (64 * i), 4 * i * RB, 0, 0);
+    }
+    if constexpr (Q8) {                                              // 16 scales: of the keys (even wavefronts) or values of half w / 2
+      const long long rs = wave / 2 ? row[1] : row[0];
+      const int n = rs < 0 ? 0 : min(16, x.len - 32 * blk - 16 * (wave / 2));
+      const float* scales = wave % 2 ? a.c.pages.v_scale : a.c.pages.k_scale;
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(scales + (rs < 0 ? 0 : rs)), 0, n * 4, 0x00020000);
+      if (lane < 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(sm.scale[stage][wave % 2] + 16 * (wave / 2)), 4, lane * 4, 0, 0, 0);
+    }
+  };
+  __builtin_amdgcn_sched_barrier(0);
+  __syncthreads();                                                   // (the piece before this one is done with LDS)
+  if (wave == 0) sm.above[lane] = mine;
+#pragma unroll 1
+  for (int i = 0; i < AHEAD; ++i) issue(blk0 + i);
+  __builtin_amdgcn_sched_barrier(0);
+
+  // ---- meanwhile the rotation
+  {
+    const double first = a.c.pos ? (double)a.c.pos0 + a.c.pos[x.b] : 0.0;
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS / 2; ++ks) {
+      double theta[8];
+      if (a.c.pos) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) theta[e] = pc_rope_theta(a.rope, 32 * ks + 8 * kk + e);
+      }
+#pragma unroll
+      for (int nc = 0; nc < NC; ++nc) {
+        u32x4 u = q[nc][ks], v = q[nc][ks + KSTEPS / 2], ul = {0, 0, 0, 0}, vl = {0, 0, 0, 0};
+        if (a.c.pos) tree_turn(u, v, ul, vl, first + (__popcll(tree_above_of(mine, node_of(nc, c16))) - 1), theta);
+        c.q[0][nc][ks] = *(bf16x8*)&u; c.q[0][nc][ks + KSTEPS / 2] = *(bf16x8*)&v;
+        c.q[1][nc][ks] = *(bf16x8*)&ul; c.q[1][nc][ks + KSTEPS / 2] = *(bf16x8*)&vl;
+      }
+    }
+  }
+
+  const int k_at = Q8 ? c16 * RB + 16 * ((kk / 2) ^ Tiles::swizzle(c16)) + 8 * (kk % 2) : c16 * RB + 16 * (kk ^ Tiles::swizzle(c16));
+  // 8 bits: a lane's VE values of its 8 keys (rows 4 kk + i, 16 + 4 kk + i), operand e of V^T is value VE d + e of row d of the
+  // result.  16 bits: reads that transpose (16 lanes point at 4 rows of 16 values, 8 bytes a lane, and get a value's 4 rows): operand e
+  // is values 16 e + d.
+  const int v_byte = VE * c16;
+  const int v_at = Q8 ? 4 * kk * RB + 16 * (v_byte / 16 ^ Tiles::swizzle(4 * kk)) + v_byte % 16
+                      : (4 * kk + c16 / 4) * RB + 16 * (c16 % 4 / 2 ^ Tiles::swizzle(4 * kk + c16 / 4)) + 8 * (c16 % 2);
+  auto block = [&](auto masked_tag, int blk, const bool (&in)[2]) __attribute__((always_inline)) {
+    constexpr bool MASKED = decltype(masked_tag)::value;
+    const int stage = (blk - blk0) & (STAGES - 1);
+    const uint8_t* ks_rows = sm.rows[stage][0];
+    const uint8_t* vs_rows = sm.rows[stage][1];
+    floatx4 s[NC][1][2];
+#pragma unroll
+    for (int nc = 0; nc < NC; ++nc)
+#pragma unroll
+      for (int bi = 0; bi < 2; ++bi) s[nc][0][bi] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < KSTEPS; ++ks)
+#pragma unroll
+      for (int bi = 0; bi < 2; ++bi) {
+        u32x4 ka;
+        if constexpr (Q8) {
+          const u32x2 w = *(const u32x2*)(ks_rows + (k_at ^ (32 * ks)) + 16 * bi * RB);
+          ka = u32x4{shared_widen(w[0], false), shared_widen(w[0], true), shared_widen(w[1], false), shared_widen(w[1], true)};
+        } else {
+          ka = *(const u32x4*)(ks_rows + (k_at ^ (64 * ks)) + 16 * bi * RB);
+        }
+#pragma unroll
+        for (int h = 1; h >= 0; --h)
+#pragma unroll
+          for (int nc = 0; nc < NC; ++nc)
+            s[nc][0][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(bf16x8*)&ka, c.q[h][nc][ks], s[nc][0][bi], 0, 0, 0);
+      }
+    __builtin_amdgcn_sched_barrier(0);                               // (every operand in flight at once has no registers)
+    vpiece vbuf[Q8 ? 8 : 1];
+    SharedScales sc[1];
+    if constexpr (Q8) {
+#pragma unroll
+      for (int bi = 0; bi < 2; ++bi) {
+        sc[0].k[bi] = *(const floatx4*)&sm.scale[stage][0][16 * bi + 4 * kk];
+        sc[0].v[bi] = *(const floatx4*)&sm.scale[stage][1][16 * bi + 4 * kk];
+      }
+    }
+    u32x4 va4[4];                                                    // four operands of V^T
+    auto value_operands = [&](int e0) __attribute__((always_inline)) {
+      if constexpr (Q8) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) va4[e] = shared_value_operand<Q8>(vbuf, e0 + e);
+      } else {
+        // (the builtin would be taken to read what is on its way to LDS, and wait for all of it)
+        const uint32_t at = (uint32_t)(uintptr_t)(lptr_t)(vs_rows + 0);
+        const uint32_t a0 = at + (v_at ^ (32 * e0)), a1 = at + (v_at ^ (32 * (e0 + 1))), a2 = at + (v_at ^ (32 * (e0 + 2))), a3 = at + (v_at ^ (32 * (e0 + 3)));
+        u32x2 r[8];
+        asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+                     "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+                     "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+                     "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\ts_waitcnt lgkmcnt(0)"
+                     : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+                     : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "n"(16 * RB) : "memory");
+#pragma unroll
+        for (int e = 0; e < 4; ++e) va4[e] = u32x4{r[2 * e][0], r[2 * e][1], r[2 * e + 1][0], r[2 * e + 1][1]};
+      }
+    };
+    const int rel = 32 * blk - x.base;
+    unsigned long long above[NC];
+    int own_kk = 0;
+    if constexpr (MASKED) {
+      const int own = tree_own(lane);
+      own_kk = own / 16;
+#pragma unroll
+      for (int nc = 0; nc < NC; ++nc) above[nc] = sm.above[node_of(nc, own % 16)];
+    }
+    const auto hidden = [&](int nc, int, int bi, int j) {
+      const int keys = in[bi] ? x.len - 32 * blk - 16 * bi : 0;
+      return !(tree_sight(above[nc], rel + 16 * bi + 4 * own_kk, min(keys, 16) - 4 * own_kk) >> j & 1);
+    };
+    u32x4 p[NC][1];
+    shared_softmax<NC, 1, VE, Q8>(s, sc, MASKED, hidden, a.scale_log2, c.ref, c.sub, c.l, c.o, p);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (Q8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        vbuf[i] = *(const vpiece*)(vs_rows + (v_at ^ (16 * (PPR == 4 ? i % 4 / 2 : i % 4))) + (i < 4 ? i : i + 12) * RB);
+    }
+    uint32_t not_finite = 0;
+#pragma unroll
+    for (int e = 0; e < VE; ++e) {
+      if (e % 4 == 0) value_operands(e);
+      u32x4 va = va4[e % 4];
+      if constexpr (MASKED) {                                        // 0 times infinity or NaN is NaN: out of the operand
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t bad = ((va[i] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((va[i] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+          va[i] &= ~bad;
+          not_finite |= bad;
+        }
+      }
+#pragma unroll
+      for (int nc = 0; nc < NC; ++nc)
+        c.o[nc][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(const bf16x8*)&va, *(const bf16x8*)&p[nc][0], c.o[nc][e], 0, 0, 0);
+    }
+    if constexpr (MASKED) {
+      if (__any(not_finite != 0)) {                                  // .. and added to the columns that see the key, value by value
+        const int own_kk = tree_own(lane) / 16;
+        uint32_t seen[NC];                                           // keys of probability above 0, of the lane's column
+#pragma unroll
+        for (int nc = 0; nc < NC; ++nc) {
+          uint32_t mine_seen = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            mine_seen |= ((p[nc][0][i] & 0x7fffu ? 1u : 0u) | (p[nc][0][i] & 0x7fff0000u ? 2u : 0u)) << (i < 2 ? 4 * own_kk + 2 * i : 12 + 4 * own_kk + 2 * i);
+          mine_seen |= (uint32_t)__shfl_xor((int)mine_seen, 16);
+          seen[nc] = mine_seen | (uint32_t)__shfl_xor((int)mine_seen, 32);
+        }
+#pragma unroll 1
+        for (int key = 0; key < 32; ++key) {
+#pragma unroll
+          for (int e = 0; e < VE; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int d = Q8 ? VE * (4 * tree_own(own_kk) + i) + e : 16 * e + 4 * tree_own(own_kk) + i, byte = d * (Q8 ? 1 : 2);
+              const uint8_t* at = vs_rows + key * RB + 16 * (byte / 16 ^ Tiles::swizzle(key)) + byte % 16;
+              const float v = Q8 ? ((*at & 0x7f) == 0x7f ? NAN : 0.f) : bf16_bits_to_f32(*(const uint16_t*)at);
+              const bool bad = !(fabsf(v) < INFINITY);
+#pragma unroll
+              for (int nc = 0; nc < NC; ++nc) c.o[nc][e][i] += bad && (seen[nc] >> key & 1) ? v : 0.f;
+            }
+        }
+      }
+    }
+  };
+  // Block `blk` has arrived when all but the wavefront's loads of the AHEAD - 1 blocks behind it have, and everybody says so; by then
+  // everybody has left the block in front of it, whose place the next one takes.
+  // Blocks that every column sees whole come first, in a loop of their own; a page that is not there ends it.
+  int blk = blk0;
+  bool in[2];
+  auto arrive = [&]() __attribute__((always_inline)) {
+    TREE_TILE_BARRIER((AHEAD - 1) * Tiles::LOADS);
+    issue(blk + AHEAD);
+    __builtin_amdgcn_sched_barrier(0);
+    in[0] = (there >> (2 * AHEAD) & 1) != 0; in[1] = (there >> (2 * AHEAD) & 2) != 0;
+    return in[0] && in[1];
+  };
+  bool whole = true;
+  for (; 32 * blk + 32 <= x.base && blk < end && (whole = arrive()); ++blk) block(std::integral_constant<bool, false>{}, blk, in);
+  for (; blk < end; ++blk) {
+    if (whole) arrive();
+    whole = true;
+    block(std::integral_constant<bool, true>{}, blk, in);
+  }
+  TREE_WAIT_LOADS(0);                                                // (nothing is on its way to LDS when the workgroup ends)
+
+  // ---- partials
+#pragma unroll
+  for (int nc = 0; nc < NC; ++nc) {
+    const float l = pc_rows_sum(c.l[nc]);
+    const int r = 16 * (NC * wave + nc) + c16;
+    if (r >= x.n_here) continue;
+    const long long row = tree_part_row(a, x, place, r);
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+    for (int u = 0; u < VE; ++u) {                                   // four values of the row at a time
+      floatx4 y;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) y[w] = l == 0.f ? 0.f : (Q8 ? c.o[nc][u % (VE / 4) * 4 + w][u / (VE / 4)] : c.o[nc][u][w]) * inv;
+      *(floatx4*)(a.part_o + row * D + (Q8 ? VE * (4 * kk + u / (VE / 4)) + u % (VE / 4) * 4 : 16 * u + 4 * kk)) = y;
+    }
+    if (kk == 0) a.part_lse[row] = l == 0.f ? -INFINITY : (c.ref[nc] + log2f(l)) * SHARED_LN2;
+  }
+}
+
 // A share's first block: of sequence begin[0], at its block begin[1].  Every thread counts the blocks of a run of sequences.
-template <typename Lds>
-__device__ __forceinline__ int tree_scan(const TreeArgs& a, int share, Lds& sm) {
+__device__ __forceinline__ int tree_scan(const TreeArgs& a, int share, TreeScanLds& sm) {
   const int lane = threadIdx.x % PC_WAVE, wave = threadIdx.x / PC_WAVE;
   const int per = (a.c.batch + TREE_THREADS - 1) / TREE_THREADS, b0 = min((int)threadIdx.x * per, a.c.batch), b1 = min(b0 + per, a.c.batch);
   int mine = 0;
@@ -329,19 +650,26 @@ __device__ __forceinline__ int tree_scan(const TreeArgs& a, int share, Lds& sm) 
   return n;
 }
 
-template <int D, int NC, int WR, bool Q8>
+// What a workgroup is: 16 or 32 query rows, each wavefront with a part of the keys; or 64 or 128, keys in LDS
+template <int D, int ROWS, bool Q8>
+struct TreeBody {
+  static constexpr bool FEW = ROWS <= 32;
+  static constexpr int NC = FEW ? ROWS / 16 : ROWS / 64;
+  typedef typename std::conditional<FEW, TreeLds<D, FEW ? NC : 1>, typename TreeTiles<D, Q8>::Lds>::type Lds;
+};
+template <int D, int ROWS, bool Q8>
 __global__ __launch_bounds__(TREE_THREADS, 2) void tree_rows_kernel(TreeArgs a) {
+  typedef TreeBody<D, ROWS, Q8> Body;
   extern __shared__ __align__(16) unsigned char lds[];
-  TreeLds<D, NC, WR>& sm = *(TreeLds<D, NC, WR>*)lds;
-  constexpr int ROWS = 16 * NC * WR;
+  typename Body::Lds& sm = *(typename Body::Lds*)lds;
   // an XCD (number mod 8) has an eighth of (share, head, tile), the tiles behind each other: its L2 serves the keys to them
   const int at = (int)(blockIdx.x % 8) * a.per_xcd + (int)(blockIdx.x / 8);
   if (at >= a.n_shares * a.c.n_kv_heads * a.n_tiles) return;
   const int sg = pc_div(at, a.tiles_div), tile = at - sg * a.n_tiles;
   const int share = pc_div(sg, a.heads_div), g = sg - share * a.c.n_kv_heads;
-  int left = tree_scan(a, share, sm);
+  int left = tree_scan(a, share, sm.scan);
   if (left == 0) return;
-  int b = __builtin_amdgcn_readfirstlane(sm.begin[0]), off = __builtin_amdgcn_readfirstlane(sm.begin[1]);
+  int b = __builtin_amdgcn_readfirstlane(sm.scan.begin[0]), off = __builtin_amdgcn_readfirstlane(sm.scan.begin[1]);
   for (; left > 0 && b < a.c.batch; ++b, off = 0) {
     const int nb = __builtin_amdgcn_readfirstlane(tree_blocks(a.c, b));
     const int take = min(left, nb - off);
@@ -357,7 +685,8 @@ __global__ __launch_bounds__(TREE_THREADS, 2) void tree_rows_kernel(TreeArgs a) 
     x.n_here = min(ROWS, n_rows * a.group - x.row0);
     if (x.n_here <= 0) continue;
     x.len = __builtin_amdgcn_readfirstlane(tree_len(a.c, b)); x.base = __builtin_amdgcn_readfirstlane(max(a.c.len[b], 0)) - n_rows;
-    tree_piece<D, NC, WR, Q8>(a, x, off, take, share + b, sm);
+    if constexpr (Body::FEW) tree_piece<D, Body::NC, Q8>(a, x, off, take, share + b, sm);
+    else tree_tile_piece<D, Body::NC, Q8>(a, x, off, take, share + b, sm);
   }
 }
 
@@ -416,7 +745,7 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, long long n_
 PcTreePlan pc_tree_plan(const PcTreeCall& c) {
   PcTreePlan p;
   const int rows = c.n * (c.n_q_heads / c.n_kv_heads);
-  p.rows = rows <= 16 ? 16 : (rows <= 32 ? 32 : 64);
+  p.rows = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128));
   p.tiles = (rows + p.rows - 1) / p.rows;
   const long long blocks = (long long)c.batch * ((((long long)c.pages.max_pages << c.pages.shift) + 31) / 32);
   long long shares = 512 / ((long long)c.n_kv_heads * p.tiles);
@@ -435,21 +764,25 @@ size_t pc_tree_ws_bytes(const PcTreeCall& c, const PcTreePlan& p) {
   return pc_align_up(rows * c.head_dim * 4, 256) + pc_align_up(rows * 4, 256) + pc_align_up((size_t)c.batch * sizeof(int2), 256);
 }
 
-template <int D, int NC, int WR, bool Q8>
+template <int D, int ROWS, bool Q8>
 static int launch_rows(const TreeArgs& a, hipStream_t st) {
   static std::atomic<uint64_t> raised{0};
-  constexpr int LDS = sizeof(TreeLds<D, NC, WR>);
-  const int rc = pc_raise_dynamic_lds((const void*)tree_rows_kernel<D, NC, WR, Q8>, LDS, raised);
+  constexpr int LDS = sizeof(typename TreeBody<D, ROWS, Q8>::Lds);
+  const int rc = pc_raise_dynamic_lds((const void*)tree_rows_kernel<D, ROWS, Q8>, LDS, raised);
   if (rc != PC_OK) return rc;
   PcProfScope prof(PC_KERNEL_TREE_ATTN, st);
-  hipLaunchKernelGGL((tree_rows_kernel<D, NC, WR, Q8>), dim3((unsigned)(8 * a.per_xcd)), dim3(TREE_THREADS), LDS, st, a);
+  hipLaunchKernelGGL((tree_rows_kernel<D, ROWS, Q8>), dim3((unsigned)(8 * a.per_xcd)), dim3(TREE_THREADS), LDS, st, a);
   PC_LAUNCH_CHECK();
   return PC_OK;
 }
 template <int D, bool Q8>
 static int launch_body(const TreeArgs& a, const PcTreePlan& p, hipStream_t st) {
-  if (p.rows == 16) return launch_rows<D, 1, 1, Q8>(a, st);
-  return p.rows == 32 ? launch_rows<D, 2, 1, Q8>(a, st) : launch_rows<D, 2, 2, Q8>(a, st);
+  switch (p.rows) {
+    case 16: return launch_rows<D, 16, Q8>(a, st);
+    case 32: return launch_rows<D, 32, Q8>(a, st);
+    case 64: return launch_rows<D, 64, Q8>(a, st);
+    default: return launch_rows<D, 128, Q8>(a, st);
+  }
 }
 template <int D>
 static int launch_all(const PcTreeCall& c, const PcTreePlan& p, void* ws, hipStream_t st) {
