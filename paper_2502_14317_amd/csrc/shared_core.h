@@ -35,9 +35,10 @@ __device__ __forceinline__ u32x4 shared_value_operand(const Piece (&v)[8], int e
 // maximum do.
 // hidden(nc, b, bi, j): is key 16 bi + 4 kk + j of block b out of column nc's sight?  Asked only where `masked`, and without a
 // branch of its own: the compiler has lost the assignment behind one with several outcomes.
+// ALL: no probability is 0 because its key is not there (0 times a scale that is not finite stays out then).
 struct SharedScales { floatx4 k[2], v[2]; };
-template <int NC, int KB, int VE, bool Q8, typename Hidden>
-__device__ __forceinline__ void shared_softmax(floatx4 (&s)[NC][KB][2], const SharedScales (&sc)[KB], bool masked, const Hidden& hidden,
+template <int NC, int KB, int VE, bool Q8, bool ALL = false, typename Scales, typename Hidden>
+__device__ __forceinline__ void shared_softmax(floatx4 (&s)[NC][KB][2], const Scales (&sc)[KB], bool masked, const Hidden& hidden,
                                                float scale_log2, float (&ref)[NC], float (&sub)[NC],
                                                float (&l)[NC], floatx4 (&o)[NC][VE], u32x4 (&p)[NC][KB]) {
   if constexpr (Q8) {
@@ -103,7 +104,7 @@ __device__ __forceinline__ void shared_softmax(floatx4 (&s)[NC][KB][2], const Sh
         }
         if constexpr (Q8) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) x[j] = x[j] == 0.f ? 0.f : x[j] * sc[b].v[bi][j];
+          for (int j = 0; j < 4; ++j) x[j] = !ALL && x[j] == 0.f ? 0.f : x[j] * sc[b].v[bi][j];
         }
         p[nc][b][2 * bi] = pack_bf16x2(x[0], x[1]);
         p[nc][b][2 * bi + 1] = pack_bf16x2(x[2], x[3]);

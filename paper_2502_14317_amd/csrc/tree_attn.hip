@@ -17,6 +17,7 @@
 #include "serve.h"
 
 #define TREE_WAVES 4
+#define TREE_EXTRA 4              // blocks that a piece costs beside its own
 #define TREE_THREADS (TREE_WAVES * PC_WAVE)
 // the N newest loads of this wavefront may still be on their way
 #define TREE_WAIT_LOADS(N) __builtin_amdgcn_s_waitcnt(0x0F70 | ((N) & 15) | (((N) >> 4) << 14))
@@ -32,7 +33,7 @@
 struct TreeArgs {
   PcTreeCall c;
   PcRope rope;
-  int group, n_tiles, n_shares, per_xcd;
+  int group, n_tiles, n_shares, per_xcd, extra;
   PcDiv group_div, tiles_div, heads_div;
   float scale_log2;
   float* part_o;           // [n_shares + B][H_kv][n group][D]
@@ -47,14 +48,20 @@ __device__ __forceinline__ int tree_own(int x) {
   return x;
 }
 
-// 32-key blocks that sequence b has: none where it has no nodes
-__device__ __forceinline__ int tree_len(const PcTreeCall& c, int b) {
-  const long long cap = (long long)c.pages.max_pages << c.pages.shift;
-  return (int)min((long long)max(c.len[b], 0), cap);
+// A sequence: its nodes, its rows with theirs (0: none; they may be more than there are places for)
+struct TreeSeq { int rows, len; };
+__device__ __forceinline__ TreeSeq tree_seq(const PcTreeCall& c, int b) {
+  TreeSeq s;
+  s.rows = c.n;
+  if (c.n_rows) s.rows = min(max(c.n_rows[b], 0), c.n);
+  s.len = max(c.len[b], 0);
+  return s;
 }
-__device__ __forceinline__ int tree_blocks(const PcTreeCall& c, int b) {
-  return pc_tree_rows(c.n_rows, b, c.n) > 0 ? (tree_len(c, b) + 31) / 32 : 0;
+// Rows that are there, and blocks of 32 of them: none where it has no nodes
+__device__ __forceinline__ int tree_there(const PcTreeCall& c, const TreeSeq& s) {
+  return (int)min((long long)s.len, (long long)c.pages.max_pages << c.pages.shift);
 }
+__device__ __forceinline__ int tree_blocks(const PcTreeCall& c, const TreeSeq& s) { return s.rows > 0 ? (tree_there(c, s) + 31) / 32 : 0; }
 
 // Which of four keys a column sees: bit j is node first + j of the tree (a row in front of it where that is negative), of which
 // `there` follow from the first one on.  No branches (a vector shift by the lane's own number costs as much as a test).
@@ -212,7 +219,7 @@ struct TreeWalk {
     const int rel = 32 * cur.blk - x.base;                   // the block's first key as a node of the tree
     const auto hidden = [&](int nc, int, int bi, int j) { return !(tree_sight(above[nc], rel + 16 * bi + 4 * kk, cur.keys[bi] - 4 * kk) >> j & 1); };
     u32x4 p[NC][1];
-    shared_softmax<NC, 1, VE, Q8>(s, sc, MASKED, hidden, a.scale_log2, c.ref, c.sub, c.l, c.o, p);
+    shared_softmax<NC, 1, VE, Q8, !MASKED>(s, sc, MASKED, hidden, a.scale_log2, c.ref, c.sub, c.l, c.o, p);
     shared_values<NC, 1, VE, MASKED>([&](int, int e) { return shared_value_operand<Q8>(vbuf, e); }, rel + 32 > 0, p, c.o);
     __builtin_amdgcn_sched_barrier(0);
     values(a, nx);
@@ -226,7 +233,7 @@ struct TreeWalk {
   }
 };
 
-struct TreeScanLds { int sums[TREE_WAVES], begin[2]; };      // of the lengths' scan
+struct TreeScanLds { int sums[TREE_WAVES], begin[2]; TreeSeq seq[TREE_THREADS]; };      // of the lengths' scan
 template <int D, int NC>
 struct TreeLds {
   SharedFewLds<D, NC, 1, TREE_WAVES> few;
@@ -301,9 +308,9 @@ __device__ __forceinline__ long long tree_part_row(const TreeArgs& a, const Tree
 template <int D, int NC, bool Q8>
 __device__ __forceinline__ void tree_piece(const TreeArgs& a, const TreePiece& x, int blk0, int n_blk, int place, TreeLds<D, NC>& sm) {
   const int lane = tree_own(threadIdx.x % PC_WAVE), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PC_WAVE);
-  const unsigned long long mine = pc_tree_above(a.c.parent, x.b, a.c.n, lane);
   TreeWalk<D, NC, Q8> walk;
   walk.begin(a, x, blk0, n_blk, wave);
+  const unsigned long long mine = pc_tree_above(a.c.parent, x.b, a.c.n, lane);
   PC_LDS_BARRIER();                                          // (the piece before this one is done with LDS)
   tree_query_rows<D, 16 * NC>(a, x, mine, sm.few.q[0], sm.few.q[1]);
   PC_LDS_BARRIER();
@@ -349,6 +356,14 @@ struct TreeTiles {
   __device__ __forceinline__ static int swizzle(int row) { return PPR == 4 ? row >> 1 & 3 : row & (PPR - 1); }
 };
 
+// A block's scales, read where they are used
+struct TreeLdsScales {
+  struct Side {
+    const float* at;
+    __device__ __forceinline__ floatx4 operator[](int bi) const { return *(const floatx4*)(at + 16 * bi); }
+  } k, v;
+};
+
 template <int D, int NC, bool Q8>
 __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePiece& x, int blk0, int n_blk, int place,
                                                 typename TreeTiles<D, Q8>::Lds& sm) {
@@ -358,7 +373,6 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
   typedef __attribute__((address_space(3))) void* lptr_t;
   const int lane = tree_own(threadIdx.x % PC_WAVE), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PC_WAVE);
   const int kk = lane / 16, c16 = lane % 16;
-  const unsigned long long mine = pc_tree_above(a.c.parent, x.b, a.c.n, lane);
   const int end = blk0 + n_blk;
 
   TreeTable tab;
@@ -376,6 +390,8 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) q[nc][ks] = *(const u32x4*)(src + 32 * ks);
   }
+  const int first_pos = a.c.pos ? a.c.pos[x.b] : 0;
+  const unsigned long long mine = pc_tree_above(a.c.parent, x.b, a.c.n, lane);
   // Waited for in front of the loads to LDS: behind those the compiler, which does not count them through the loop, waits for too many
   asm volatile("" : "+v"(tab.here), "+v"(tab.next));
 #pragma unroll
@@ -388,6 +404,7 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
   const int my_half = RB >= 128 ? wave / 2 : wave % 2, row0 = RB >= 128 ? 8 * wave : 16 * (wave % 2);      // (of the block)
   const int at_row = row0 % 16 + lane / PPR;                         // of the half
   const int off = at_row * RB + 16 * (lane % PPR ^ Tiles::swizzle(at_row));
+  int to = 0, from = 0;                                              // the next block's stage, the one at hand's
   uint32_t there = 0;                                                // two bits a block: are the halves' pages there
   auto issue = [&](int blk) __attribute__((always_inline)) {
     long long row[2];
@@ -397,7 +414,8 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
       row[h] = blk < end && key < x.len ? tab.row(a, x, key) : -1;
     }
     there = there << 2 | (row[0] >= 0 ? 1u : 0u) | (row[1] >= 0 ? 2u : 0u);
-    const int stage = (blk - blk0) & (STAGES - 1);
+    const int stage = to;
+    to = to + 1 == STAGES ? 0 : to + 1;
     const long long r = my_half ? row[1] : row[0];
     const int keys = r < 0 ? 0 : min(16, x.len - 32 * blk - 16 * my_half);
     const long long at = r < 0 ? 0 : r;
@@ -407,7 +425,7 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
       const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)(kv ? a.c.pages.v : a.c.pages.k) + at * RB), 0, keys * RB, 0x00020000);
 #pragma unroll
       for (int i = 0; i < (RB == 256 ? 2 : 1); ++i)                  // (rows 4 further on: another bit of the swizzle)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(sm.rows[stage][kv] + (row0 + 4 * i) * RB), 16, off ^ (64 * i), 4 * i * RB, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(sm.rows[stage][kv] + (row0 + 4 * i) * RB), 16, off ^ (64 * i), 4 * i * RB, 0, NC == 1 ? PC_BUF_NT : 0);
     }
     if constexpr (Q8) {                                              // 16 scales: of the keys (even wavefronts) or values of half w / 2
       const long long rs = wave / 2 ? row[1] : row[0];
@@ -426,7 +444,7 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
 
   // ---- meanwhile the rotation
   {
-    const double first = a.c.pos ? (double)a.c.pos0 + a.c.pos[x.b] : 0.0;
+    const double first = (double)a.c.pos0 + first_pos;
 #pragma unroll
     for (int ks = 0; ks < KSTEPS / 2; ++ks) {
       double theta[8];
@@ -453,7 +471,8 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
                       : (4 * kk + c16 / 4) * RB + 16 * (c16 % 4 / 2 ^ Tiles::swizzle(4 * kk + c16 / 4)) + 8 * (c16 % 2);
   auto block = [&](auto masked_tag, int blk, const bool (&in)[2]) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked_tag)::value;
-    const int stage = (blk - blk0) & (STAGES - 1);
+    const int stage = from;
+    from = from + 1 == STAGES ? 0 : from + 1;
     const uint8_t* ks_rows = sm.rows[stage][0];
     const uint8_t* vs_rows = sm.rows[stage][1];
     floatx4 s[NC][1][2];
@@ -480,14 +499,7 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
       }
     __builtin_amdgcn_sched_barrier(0);                               // (every operand in flight at once has no registers)
     vpiece vbuf[Q8 ? 8 : 1];
-    SharedScales sc[1];
-    if constexpr (Q8) {
-#pragma unroll
-      for (int bi = 0; bi < 2; ++bi) {
-        sc[0].k[bi] = *(const floatx4*)&sm.scale[stage][0][16 * bi + 4 * kk];
-        sc[0].v[bi] = *(const floatx4*)&sm.scale[stage][1][16 * bi + 4 * kk];
-      }
-    }
+    const TreeLdsScales sc[1] = {{{sm.scale[stage][0] + 4 * kk}, {sm.scale[stage][1] + 4 * kk}}};
     u32x4 va4[4];                                                    // four operands of V^T
     auto value_operands = [&](int e0) __attribute__((always_inline)) {
       if constexpr (Q8) {
@@ -522,7 +534,7 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
       return !(tree_sight(above[nc], rel + 16 * bi + 4 * own_kk, min(keys, 16) - 4 * own_kk) >> j & 1);
     };
     u32x4 p[NC][1];
-    shared_softmax<NC, 1, VE, Q8>(s, sc, MASKED, hidden, a.scale_log2, c.ref, c.sub, c.l, c.o, p);
+    shared_softmax<NC, 1, VE, Q8, !MASKED>(s, sc, MASKED, hidden, a.scale_log2, c.ref, c.sub, c.l, c.o, p);
     __builtin_amdgcn_sched_barrier(0);
     if constexpr (Q8) {
 #pragma unroll
@@ -616,12 +628,18 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
   }
 }
 
-// A share's first block: of sequence begin[0], at its block begin[1].  Every thread counts the blocks of a run of sequences.
+// A share's first place on the line of all sequences' blocks: of sequence begin[0], at its begin[1].  In front of a sequence's
+// blocks are `extra` places without one, for what a piece costs beside its keys.  Every thread counts those of a run of sequences.
 __device__ __forceinline__ int tree_scan(const TreeArgs& a, int share, TreeScanLds& sm) {
   const int lane = threadIdx.x % PC_WAVE, wave = threadIdx.x / PC_WAVE;
   const int per = (a.c.batch + TREE_THREADS - 1) / TREE_THREADS, b0 = min((int)threadIdx.x * per, a.c.batch), b1 = min(b0 + per, a.c.batch);
+  auto places = [&](const TreeSeq& s) { const int nb = tree_blocks(a.c, s); return nb > 0 ? nb + a.extra : 0; };
   int mine = 0;
-  for (int b = b0; b < b1; ++b) mine += tree_blocks(a.c, b);
+  for (int b = b0; b < b1; ++b) {
+    const TreeSeq s = tree_seq(a.c, b);
+    if (per == 1) sm.seq[b] = s;
+    mine += places(s);
+  }
   const int incl = pc_wave_scan(mine);
   if (lane == PC_WAVE - 1) sm.sums[wave] = incl;
   __syncthreads();
@@ -634,15 +652,15 @@ __device__ __forceinline__ int tree_scan(const TreeArgs& a, int share, TreeScanL
   // shares as equal as possible, of 8 blocks at least
   const int n_eff = max(1, min(a.n_shares, total / 8));
   if (share >= n_eff) return 0;
-  const int each = total / n_eff, extra = total - each * n_eff;
-  const int lo = share * each + min(share, extra), n = each + (share < extra);
+  const int each = total / n_eff, rest = total - each * n_eff;
+  const int lo = share * each + min(share, rest), n = each + (share < rest);
   if (n == 0) return 0;
   if (lo >= before && lo < before + mine) {
     int off = lo - before, b = b0;
     for (; b < b1; ++b) {
-      const int nb = tree_blocks(a.c, b);
-      if (off < nb) break;
-      off -= nb;
+      const int p = places(tree_seq(a.c, b));
+      if (off < p) break;
+      off -= p;
     }
     sm.begin[0] = b; sm.begin[1] = off;
   }
@@ -671,22 +689,27 @@ __global__ __launch_bounds__(TREE_THREADS, 2) void tree_rows_kernel(TreeArgs a) 
   if (left == 0) return;
   int b = __builtin_amdgcn_readfirstlane(sm.scan.begin[0]), off = __builtin_amdgcn_readfirstlane(sm.scan.begin[1]);
   for (; left > 0 && b < a.c.batch; ++b, off = 0) {
-    const int nb = __builtin_amdgcn_readfirstlane(tree_blocks(a.c, b));
-    const int take = min(left, nb - off);
-    if (take <= 0) continue;
+    TreeSeq s;
+    if (a.c.batch <= TREE_THREADS) s = sm.scan.seq[b];
+    else s = tree_seq(a.c, b);
+    s.rows = __builtin_amdgcn_readfirstlane(s.rows); s.len = __builtin_amdgcn_readfirstlane(s.len);
+    const int nb = tree_blocks(a.c, s);
+    if (nb == 0) continue;
+    const int take = min(left, nb + a.extra - off);
     left -= take;
+    const int blk0 = max(off - a.extra, 0), n_blk = max(off + take - a.extra, 0) - blk0;
+    if (n_blk == 0) continue;
     if (g == 0 && tile == 0 && threadIdx.x == 0) {
-      if (off == 0) a.span[b].x = share;
-      if (off + take == nb) a.span[b].y = share;
+      if (blk0 == 0) a.span[b].x = share;
+      if (blk0 + n_blk == nb) a.span[b].y = share;
     }
     TreePiece x;
     x.b = b; x.g = g; x.row0 = tile * ROWS;
-    const int n_rows = __builtin_amdgcn_readfirstlane(pc_tree_rows(a.c.n_rows, b, a.c.n));
-    x.n_here = min(ROWS, n_rows * a.group - x.row0);
+    x.n_here = min(ROWS, s.rows * a.group - x.row0);
     if (x.n_here <= 0) continue;
-    x.len = __builtin_amdgcn_readfirstlane(tree_len(a.c, b)); x.base = __builtin_amdgcn_readfirstlane(max(a.c.len[b], 0)) - n_rows;
-    if constexpr (Body::FEW) tree_piece<D, Body::NC, Q8>(a, x, off, take, share + b, sm);
-    else tree_tile_piece<D, Body::NC, Q8>(a, x, off, take, share + b, sm);
+    x.len = tree_there(a.c, s); x.base = s.len - s.rows;
+    if constexpr (Body::FEW) tree_piece<D, Body::NC, Q8>(a, x, blk0, n_blk, share + b, sm);
+    else tree_tile_piece<D, Body::NC, Q8>(a, x, blk0, n_blk, share + b, sm);
   }
 }
 
@@ -699,11 +722,12 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, long long n_
   if (row >= n_out) return;
   const int bt = pc_div((int)row, heads_div), h = (int)row - bt * a.c.n_q_heads;
   const int b = pc_div(bt, nodes_div), t = bt - b * a.c.n;
-  if (t >= pc_tree_rows(a.c.n_rows, b, a.c.n)) return;
+  const TreeSeq seq = tree_seq(a.c, b);
+  if (t >= seq.rows) return;
   const int g = pc_div(h, a.group_div), r = t * a.group + h - g * a.group;
   float m = -INFINITY, den = 0.f;
   floatx4 num = {0.f, 0.f, 0.f, 0.f};
-  if (tree_blocks(a.c, b) > 0) {
+  if (tree_blocks(a.c, seq) > 0) {
     const int2 span = a.span[b];
     for (int s0 = span.x; s0 <= span.y; s0 += U) {
       float l[U];
@@ -756,7 +780,7 @@ PcTreePlan pc_tree_plan(const PcTreeCall& c) {
 static long long workgroups(const PcTreeCall& c, const PcTreePlan& p) { return (long long)p.shares * c.n_kv_heads * p.tiles; }
 bool pc_tree_fits(const PcTreeCall& c, const PcTreePlan& p) {
   const long long blocks = (((long long)c.pages.max_pages << c.pages.shift) + 31) / 32;
-  return workgroups(c, p) < (1LL << 32) / TREE_THREADS - 8 && c.batch * blocks < (1LL << 31);
+  return workgroups(c, p) < (1LL << 32) / TREE_THREADS - 8 && c.batch * (blocks + TREE_EXTRA) < (1LL << 31);
 }
 static size_t part_rows(const PcTreeCall& c, const PcTreePlan& p) { return (size_t)(p.shares + c.batch) * c.n * c.n_q_heads; }
 size_t pc_tree_ws_bytes(const PcTreeCall& c, const PcTreePlan& p) {
@@ -790,7 +814,7 @@ static int launch_all(const PcTreeCall& c, const PcTreePlan& p, void* ws, hipStr
   a.c = c;
   a.rope = pc_rope_factors(c.pos ? c.rope_base : 2.0f, c.head_dim);
   a.group = c.n_q_heads / c.n_kv_heads; a.n_tiles = p.tiles; a.n_shares = p.shares;
-  a.per_xcd = (int)((workgroups(c, p) + 7) / 8);
+  a.per_xcd = (int)((workgroups(c, p) + 7) / 8); a.extra = TREE_EXTRA;
   a.group_div = pc_div_by(a.group); a.tiles_div = pc_div_by(p.tiles); a.heads_div = pc_div_by(c.n_kv_heads);
   a.scale_log2 = c.scale * SHARED_LOG2E;
   const size_t rows = part_rows(c, p);
