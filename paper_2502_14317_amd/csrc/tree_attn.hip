@@ -96,6 +96,15 @@ struct TreeTable {
     here = entries(a, x, at);
     next = entries(a, x, at + PC_WAVE);
   }
+  // are all the pages of entries lo .. hi there?
+  __device__ __forceinline__ bool all(const TreeArgs& a, const TreePiece& x, int lo, int hi) const {
+    bool there = true;
+    for (int at = lo; at <= hi; at += PC_WAVE) {
+      const int page = at == lo ? here : entries(a, x, at);
+      there &= at + (int)(threadIdx.x % PC_WAVE) > hi || (uint32_t)page < (uint32_t)a.c.pages.n_pages;
+    }
+    return __all(there);
+  }
   // the row of the pool where key `key` lies, -1 if it is not there; keys are asked for in order
   __device__ __forceinline__ long long row(const TreeArgs& a, const TreePiece& x, int key) {
     const int at = key >> a.c.pages.shift;
@@ -116,7 +125,7 @@ struct TreeWalk {
   vpiece vbuf[8];
   float sbuf;
   TreeBlock cur;
-  int end;                                                   // the run's last block is in front of it
+  int whole_end, end;                                        // of the blocks that every column sees whole, of the run
   TreeTable tab;
 
   __device__ __forceinline__ TreeBlock block(const TreeArgs& a, const TreePiece& x, int blk) {
@@ -166,6 +175,8 @@ struct TreeWalk {
     const int first = blk0 + (int)((long long)n_blk * wave / TREE_WAVES);
     end = blk0 + (int)((long long)n_blk * (wave + 1) / TREE_WAVES);
     tab.begin(a, x, (32 * first) >> a.c.pages.shift);
+    whole_end = first < end && tab.all(a, x, (32 * first) >> a.c.pages.shift, (min(32 * end, x.len) - 1) >> a.c.pages.shift)
+                    ? min(end, max(x.base, 0) / 32) : first;
     cur = block(a, x, first);
     keys(a, cur);
     values(a, cur);
@@ -225,10 +236,11 @@ struct TreeWalk {
     values(a, nx);
     cur = nx;
   }
-  // above: the nodes that the lane's columns see, as bits.  The blocks that every column sees whole come first.
+  // above: the nodes that the lane's columns see, as bits.  The blocks that every column sees whole come first (none where one of
+  // the run's pages is not there).
   __device__ __forceinline__ void run(const TreeArgs& a, const TreePiece& x, SharedColumns<D, NC>& c, const unsigned long long (&above)[NC], float (*scale)[32],
                                       const uint16_t (*hi)[D + 8], const uint16_t (*lo)[D + 8]) {
-    while (cur.keys[0] == 16 && cur.keys[1] == 16 && 32 * cur.blk + 32 <= x.base) step<false>(a, x, c, above, scale, hi, lo);
+    while (cur.blk < whole_end) step<false>(a, x, c, above, scale, hi, lo);
     while (cur.blk < end) step<true>(a, x, c, above, scale, hi, lo);
   }
 };
@@ -377,6 +389,7 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
 
   TreeTable tab;
   tab.begin(a, x, (32 * blk0) >> a.c.pages.shift);
+  const bool all_there = tab.all(a, x, (32 * blk0) >> a.c.pages.shift, (min(32 * end, x.len) - 1) >> a.c.pages.shift);
 
   // ---- the wavefront's query rows, as they lie in the operands: both values of a pair are the same lane's
   SharedColumns<D, NC> c;
@@ -590,21 +603,22 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
   };
   // Block `blk` has arrived when all but the wavefront's loads of the AHEAD - 1 blocks behind it have, and everybody says so; by then
   // everybody has left the block in front of it, whose place the next one takes.
-  // Blocks that every column sees whole come first, in a loop of their own; a page that is not there ends it.
-  int blk = blk0;
-  bool in[2];
-  auto arrive = [&]() __attribute__((always_inline)) {
+  // Blocks that every column sees whole come first, in a loop of their own (none where one of the piece's pages is not there).
+  const int whole_end = all_there ? min(end, max(x.base, 0) / 32) : blk0;
+  auto arrive = [&](int blk) __attribute__((always_inline)) {
     TREE_TILE_BARRIER((AHEAD - 1) * Tiles::LOADS);
     issue(blk + AHEAD);
     __builtin_amdgcn_sched_barrier(0);
-    in[0] = (there >> (2 * AHEAD) & 1) != 0; in[1] = (there >> (2 * AHEAD) & 2) != 0;
-    return in[0] && in[1];
   };
-  bool whole = true;
-  for (; 32 * blk + 32 <= x.base && blk < end && (whole = arrive()); ++blk) block(std::integral_constant<bool, false>{}, blk, in);
+  int blk = blk0;
+  for (; blk < whole_end; ++blk) {
+    arrive(blk);
+    const bool in[2] = {true, true};
+    block(std::integral_constant<bool, false>{}, blk, in);
+  }
   for (; blk < end; ++blk) {
-    if (whole) arrive();
-    whole = true;
+    arrive(blk);
+    const bool in[2] = {(there >> (2 * AHEAD) & 1) != 0, (there >> (2 * AHEAD) & 2) != 0};
     block(std::integral_constant<bool, true>{}, blk, in);
   }
   TREE_WAIT_LOADS(0);                                                // (nothing is on its way to LDS when the workgroup ends)
