@@ -1,7 +1,7 @@
 // What the tokens of a vocabulary are worth: one pass over a row of logits x keeps, relative to a running maximum m in log2
 // units, l = sum 2^(x - m) and e = sum 2^(x - m) (x - m), from which with L = log2 l
 //   log2 p(v) = x_v - m - L,   entropy / ln 2 = L - e / l.
-// A term of x = -inf is 0 (its factor is held above -1e4, and 2^-1e4 is 0); NaN and +inf make l NaN, and with it every number
+// A term of x = -inf is 0 (where one is met its factor is held above -1e4, and 2^-1e4 is 0); NaN and +inf make l NaN, and with it every number
 // of the row.
 // The n_top largest: the pass knows the largest logit of every thread.  With the j-th largest of those in each of F
 // wavefronts, F j >= n_top, the least of the F is one that n_top logits at least reach, and few more do (20 of 128256: some 70).
@@ -10,7 +10,7 @@
 // the n_top-th of the order (logit, token) is found eight bits at a time.
 #include "paged.h"
 
-#define LOGPROBS_THREADS 1024
+#define LOGPROBS_THREADS 512
 #define LOGPROBS_WAVES (LOGPROBS_THREADS / PC_WAVE)
 #define LOGPROBS_LOG2E 1.4426950408889634f
 #define LOGPROBS_LN2 0.6931471805599453f
@@ -29,7 +29,8 @@ struct TopLds {
   top_key key[TOP_LIST];
   int count, threads;
   uint16_t thread[LOGPROBS_THREADS];
-  uint32_t wave[LOGPROBS_WAVES];
+  __align__(16) uint32_t wave[2 * PC_WAVE + 4];
+  uint32_t reach;
   int digits[256];
 };
 
@@ -52,21 +53,25 @@ struct LogSum {
     l += y.l;
     e += y.e;
   }
-  // returns the largest of them
-  template <int N>
-  __device__ __forceinline__ float add(const float (&x)[N]) {
-    float most = x[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) most = fmaxf(most, x[i]);
-    if (most * LOGPROBS_LOG2E > m) move(most * LOGPROBS_LOG2E);        // (log2 e > 0: the maximum commutes with it)
+  // N logits; largest: of them.  (A wavefront whose references stay, most of them, passes by the move.)  e is left to the caller: the
+  // terms' sum is returned.  HELD: their factors are held above -1e4, and what is known of l stays
+  template <int N, bool HELD = false>
+  __device__ __forceinline__ float add(const float (&x)[N], float largest) {
+    if constexpr (!HELD) {
+      const float top = largest * LOGPROBS_LOG2E;           // (log2 e > 0: the maximum commutes with it)
+      if (__any(top > m)) {
+        if (top > m) move(top);
+      }
+    }
     const float ref = m == -INFINITY ? 0.f : m;
+    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float t = fmaf(x[i], LOGPROBS_LOG2E, -ref), p = __builtin_amdgcn_exp2f(t);
-      l += p;
-      e = fmaf(p, fmaxf(t, -1e4f), e);
+      if constexpr (!HELD) l += p;
+      sum = fmaf(p, HELD ? fmaxf(t, -1e4f) : t, sum);
     }
-    return most;
+    return sum;
   }
   __device__ __forceinline__ float logprob(float x) const { return (fmaf(x, LOGPROBS_LOG2E, -m) - log2f(l)) * LOGPROBS_LN2; }
   __device__ __forceinline__ float entropy() const { return (log2f(l) - e / l) * LOGPROBS_LN2; }
@@ -107,6 +112,10 @@ struct LogprobsRow {
     }
   }
   __device__ __forceinline__ u32x4 piece(int i) const { return *(const u32x4*)(p + head + (long long)i * VE); }
+  __device__ __forceinline__ static u32x4 nothing() {        // a piece of -inf
+    const uint32_t w = VE == 8 ? 0xff80ff80u : 0xff800000u;
+    return u32x4{w, w, w, w};
+  }
   // f(value, token) for the element of the head or tail that is the thread's, if there is one
   template <typename F>
   __device__ __forceinline__ void edges(F f) const {
@@ -135,22 +144,48 @@ __device__ __forceinline__ top_key top_block_max(top_key x) {
   for (int w = 1; w < THREADS / PC_WAVE; ++w) x = red[w] > x ? red[w] : x;
   return x;
 }
+// Over the wavefront's lanes, left in the last one: rows of 16 by shifts, then row after row
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float sum_from(float x, float none) {
+  return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp((int)__float_as_uint(none), (int)__float_as_uint(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float sum_wave_max(float x) {
+  x = fmaxf(x, sum_from<0x111, 0xf>(x, -INFINITY));         // row_shr: 1, 2, 4, 8
+  x = fmaxf(x, sum_from<0x112, 0xf>(x, -INFINITY));
+  x = fmaxf(x, sum_from<0x114, 0xf>(x, -INFINITY));
+  x = fmaxf(x, sum_from<0x118, 0xf>(x, -INFINITY));
+  x = fmaxf(x, sum_from<0x142, 0xa>(x, -INFINITY));         // row_bcast: 15, 31
+  return fmaxf(x, sum_from<0x143, 0xc>(x, -INFINITY));
+}
+__device__ __forceinline__ float sum_wave(float x) {
+  x += sum_from<0x111, 0xf>(x, 0.f);
+  x += sum_from<0x112, 0xf>(x, 0.f);
+  x += sum_from<0x114, 0xf>(x, 0.f);
+  x += sum_from<0x118, 0xf>(x, 0.f);
+  x += sum_from<0x142, 0xa>(x, 0.f);
+  return x + sum_from<0x143, 0xc>(x, 0.f);
+}
 template <int THREADS>
 __device__ __forceinline__ LogSum sum_block(LogSum s) {
   __shared__ LogSum red[THREADS / PC_WAVE];
+  s.move(__uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(sum_wave_max(s.m)), PC_WAVE - 1)));
+  s.l = sum_wave(s.l);
+  s.e = sum_wave(s.e);
+  __syncthreads();
+  if (threadIdx.x % PC_WAVE == PC_WAVE - 1) red[threadIdx.x / PC_WAVE] = s;
+  __syncthreads();
+  LogSum all;                                               // (each wavefront's relative to the largest: nothing waits for the one before)
+  all.clear();
 #pragma unroll
-  for (int off = 1; off < PC_WAVE; off <<= 1) {
-    LogSum y;
-    y.m = __shfl_xor(s.m, off); y.l = __shfl_xor(s.l, off); y.e = __shfl_xor(s.e, off);
-    s.join(y);                                              // (lane 0's sum is the one that counts)
+  for (int w = 0; w < THREADS / PC_WAVE; ++w) all.m = fmaxf(all.m, red[w].m);
+#pragma unroll
+  for (int w = 0; w < THREADS / PC_WAVE; ++w) {
+    LogSum y = red[w];
+    y.move(all.m);
+    all.l += y.l;
+    all.e += y.e;
   }
-  __syncthreads();
-  if (threadIdx.x % PC_WAVE == 0) red[threadIdx.x / PC_WAVE] = s;
-  __syncthreads();
-  s = red[0];
-#pragma unroll
-  for (int w = 1; w < THREADS / PC_WAVE; ++w) s.join(red[w]);
-  return s;
+  return all;
 }
 
 // What a row's caller gets, from its sum and its top list (LDS or the list's keys in order)
@@ -182,34 +217,62 @@ __device__ __forceinline__ uint32_t top_wave_max(uint32_t x) {
   return max(max((uint32_t)__builtin_amdgcn_readlane((int)x, 15), (uint32_t)__builtin_amdgcn_readlane((int)x, 31)),
              max((uint32_t)__builtin_amdgcn_readlane((int)x, 47), (uint32_t)__builtin_amdgcn_readlane((int)x, 63)));
 }
-// A key that at least n_top of the threads' largest reach (0: every key does); full: wavefronts all of whose threads have one
+// A key that at least n_top of the threads' largest reach (0: every key does): of each full wavefront's (all of its threads have
+// one) j largest, which are n_top together and a few more, the n_top-th.
 __device__ __forceinline__ uint32_t top_reach(uint32_t mine, int n_top, int full, TopLds& sm) {
   const int lane = threadIdx.x % PC_WAVE, wave = threadIdx.x / PC_WAVE;
   if (full == 0) return 0;
-  uint32_t x = mine, jth = 0;
-  for (int j = 0; j < n_top; j += full) {                   // (uniform)
-    jth = top_wave_max(x);
-    const unsigned long long has = __ballot(x == jth);
-    if (lane == __ffsll((long long)has) - 1) x = 0;
+  const int most = min((n_top + full - 1) / full + 3, PC_WAVE), n = most * full;       // 128 at most
+  if (wave < full) {
+    uint32_t x = mine, out = 0;
+    for (int j = 0; j < most; ++j) {                        // (uniform)
+      const uint32_t jth = top_wave_max(x);
+      const unsigned long long has = __ballot(x == jth);
+      if (lane == __ffsll((long long)has) - 1) x = 0;
+      if (lane == j) out = jth;
+    }
+    if (lane < most) sm.wave[wave * most + lane] = out;
   }
-  if (lane == 0) sm.wave[wave] = jth;
+  if (threadIdx.x < 4) sm.wave[n + threadIdx.x] = 0;        // (read with the last ones)
   __syncthreads();
-  uint32_t least = ~0u;
-  for (int w = 0; w < full; ++w) least = min(least, sm.wave[w]);
-  return least;
+  if (wave == 0) {                                          // the least of those that fewer than n_top are above
+    const uint32_t a = lane < n ? sm.wave[lane] : 0, b = lane + PC_WAVE < n ? sm.wave[lane + PC_WAVE] : 0;
+    int above_a = 0, above_b = 0;
+#pragma unroll 4
+    for (int i = 0; i < n; i += 4) {
+      const u32x4 x = *(const u32x4*)&sm.wave[i];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        above_a += x[u] > a;
+        above_b += x[u] > b;
+      }
+    }
+    const uint32_t in_a = lane < n && above_a < n_top ? ~a : 0, in_b = lane + PC_WAVE < n && above_b < n_top ? ~b : 0;
+    const uint32_t least = ~top_wave_max(max(in_a, in_b));
+    if (lane == 0) sm.reach = least;
+  }
+  __syncthreads();
+  return sm.reach;
 }
 __device__ __forceinline__ void top_push(TopLds& sm, top_key k) {
   const int at = atomicAdd(&sm.count, 1);
   if (at < TOP_LIST) sm.key[at] = k;
 }
-// f(place, key) for the list's n_top first in order; the list has no key twice
+// f(place, key) for the list's n_top first in order; the list has no key twice.  Eight threads a key, each with an eighth of the
+// others.
 template <int THREADS, typename F>
 __device__ __forceinline__ void top_in_order(const TopLds& sm, int count, int n_top, F f) {
-  for (int i = threadIdx.x; i < count; i += THREADS) {
-    const top_key mine = sm.key[i];
+  const int eighth = threadIdx.x % 8;
+  for (int i0 = 0; i0 < count; i0 += THREADS / 8) {
+    const int i = i0 + (int)threadIdx.x / 8;
+    const top_key mine = sm.key[min(i, count - 1)];
     int before = 0;
-    for (int c = 0; c < count; ++c) before += sm.key[c] > mine;
-    if (before < n_top) f(before, mine);
+#pragma unroll 4
+    for (int c = eighth; c < count; c += 8) before += sm.key[c] > mine;
+    before += __shfl_xor(before, 1);
+    before += __shfl_xor(before, 2);
+    before += __shfl_xor(before, 4);
+    if (i < count && eighth == 0 && before < n_top) f(before, mine);
   }
 }
 
@@ -267,14 +330,24 @@ __device__ __forceinline__ void top_of_part(const LogprobsRow<T>& r, float large
   r.edges([&](float x, int v) { if (pc_order_key(x) >= reach) top_push(sm, top_key_of(x, v)); });
   __syncthreads();
   const int threads = sm.threads, rounds = (n + LOGPROBS_THREADS - 1) / LOGPROBS_THREADS;
-  for (int j = threadIdx.x; j < threads * rounds; j += LOGPROBS_THREADS) {
-    const int round = j / threads, i = r.lo + round * LOGPROBS_THREADS + sm.thread[j - round * threads];
-    if (i >= r.hi) continue;
-    float x[VE];
-    LogprobsRow<T>::values(r.piece(i), x);
+  for (int j0 = threadIdx.x; j0 < threads * rounds; j0 += 2 * LOGPROBS_THREADS) {
+    u32x4 w[2];
+    int i[2];
 #pragma unroll
-    for (int e = 0; e < VE; ++e)
-      if (pc_order_key(x[e]) >= reach) top_push(sm, top_key_of(x[e], r.head + i * VE + e));
+    for (int u = 0; u < 2; ++u) {
+      const int j = j0 + u * LOGPROBS_THREADS, round = j / threads;
+      i[u] = j < threads * rounds ? r.lo + round * LOGPROBS_THREADS + sm.thread[j - round * threads] : r.hi;
+      w[u] = i[u] < r.hi ? r.piece(i[u]) : LogprobsRow<T>::nothing();
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if (i[u] >= r.hi) continue;
+      float x[VE];
+      LogprobsRow<T>::values(w[u], x);
+#pragma unroll
+      for (int e = 0; e < VE; ++e)
+        if (pc_order_key(x[e]) >= reach) top_push(sm, top_key_of(x[e], r.head + i[u] * VE + e));
+    }
   }
   __syncthreads();
   int count = sm.count;
@@ -304,24 +377,46 @@ __global__ __launch_bounds__(LOGPROBS_THREADS) void logprobs_rows_kernel(Logprob
     u32x4 w[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) w[u] = r.piece(min(i0 + u * LOGPROBS_THREADS, r.hi - 1));
+    float x[U * VE], top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (i0 + u * LOGPROBS_THREADS >= r.hi) break;
-      float x[VE];
-      LogprobsRow<T>::values(w[u], x);
-      largest = fmaxf(largest, s.add(x));
+      if (i0 + u * LOGPROBS_THREADS >= r.hi) w[u] = LogprobsRow<T>::nothing();
+      float y[VE];
+      LogprobsRow<T>::values(w[u], y);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) x[u * VE + e] = y[e];
+#pragma unroll
+      for (int e = 0; e < VE; e += 2) top = fmaxf(fmaxf(top, x[u * VE + e]), x[u * VE + e + 1]);
     }
+    float terms = s.add(x, top);
+    if (__any(terms != terms)) {                            // a logit of -inf, or worse: once more, from the caches
+      terms = 0.f;
+#pragma unroll 1
+      for (int i = i0; i < min(i0 + U * LOGPROBS_THREADS, r.hi); i += LOGPROBS_THREADS) {
+        float y[VE];
+        LogprobsRow<T>::values(r.piece(i), y);
+        terms += s.template add<VE, true>(y, 0.f);
+      }
+    }
+    s.e += terms;
+    largest = fmaxf(largest, top);
   }
-  r.edges([&](float x, int) { const float one[1] = {x}; s.add(one); });
+  r.edges([&](float x, int) {
+    const float one[1] = {x};
+    s.add(one, x);
+    s.e += s.template add<1, true>(one, x);
+  });
   s = sum_block<LOGPROBS_THREADS>(s);
   if (a.parts == 1) logprobs_out<T>(a.c, row, s);
   else if (threadIdx.x == 0) a.sums[blockIdx.x] = s;
   if (a.c.n_top == 0) return;
-  if (a.parts == 1) top_of_part(r, largest, a.c.n_top, sm, [&](int i, top_key k) { logprobs_top_out(a.c, row, s, i, k); });
-  else top_of_part(r, largest, a.c.n_top, sm, [&](int i, top_key k) { a.tops[(long long)blockIdx.x * a.c.n_top + i] = k; });
+  top_of_part(r, largest, a.c.n_top, sm, [&](int i, top_key k) {
+    if (a.parts == 1) logprobs_top_out(a.c, row, s, i, k);
+    else a.tops[(long long)blockIdx.x * a.c.n_top + i] = k;
+  });
 }
 
-// A row's parts, joined.  The largest of the parts' n_top-th keys is one that n_top keys reach.
+// A row's parts, joined.  n_top keys reach the least of the parts' j-th ones, n_top <= j parts, and the largest of their n_top-th
 #define JOIN_THREADS 256
 template <typename T>
 __global__ __launch_bounds__(JOIN_THREADS) void logprobs_join_kernel(LogprobsArgs a) {
@@ -335,12 +430,16 @@ __global__ __launch_bounds__(JOIN_THREADS) void logprobs_join_kernel(LogprobsArg
   logprobs_out<T>(a.c, row, s);
   if (n_top == 0) return;
   const top_key* tops = a.tops + row * a.parts * n_top;
-  top_key reach = 1;                                        // (0 is nobody)
+  const int jth = (n_top + a.parts - 1) / a.parts;
+  top_key last = 1, least = ~0ull;                          // (0 is nobody)
   for (int i = threadIdx.x; i < a.parts; i += JOIN_THREADS) {
-    const top_key k = tops[(long long)i * n_top + n_top - 1];
-    reach = k > reach ? k : reach;
+    const top_key k = tops[(long long)i * n_top + n_top - 1], j = tops[(long long)i * n_top + jth - 1];
+    last = k > last ? k : last;
+    least = j < least ? j : least;
   }
-  reach = top_block_max<JOIN_THREADS>(reach);
+  last = top_block_max<JOIN_THREADS>(last);
+  least = ~top_block_max<JOIN_THREADS>(~least);
+  const top_key reach = least > last ? least : last;
   if (threadIdx.x == 0) sm.count = 0;
   __syncthreads();
   for (int i = threadIdx.x; i < a.parts * n_top; i += JOIN_THREADS) {
