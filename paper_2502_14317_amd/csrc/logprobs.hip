@@ -463,12 +463,19 @@ __global__ __launch_bounds__(JOIN_THREADS) void logprobs_join_kernel(LogprobsArg
 }
 
 // ---- host
-static int logprobs_parts(int rows, int vocab) {
-  const int parts = 512 / (rows < 1 ? 1 : rows), most = vocab / 4096;
-  return parts < 1 || most < 1 ? 1 : (parts < most ? parts : most);
+// Workgroups a row: one, in one launch, but for few rows of more than 192 KB, which are cut into about 256 parts in all, of 16 KB at
+// least.  us a call, one / 256 parts in all, 5 of the largest asked for:
+//   bf16 (16 x 32000) 8.4 / 11.4   (16 x 64000) 9.8 / 11.6   (4 x 128256) 13.3 / 11.8   (64 x 128256) 14.0 / 13.2   (128 x 128256) 15.0 / 15.5
+//   fp32 (16 x 32000) 7.9 / 10.7   (64 x 64000) 10.2 / 11.8  (4 x 128256) 14.0 / 11.2   (64 x 128256) 17.4 / 13.9   (128 x 128256) 18.3 / 19.6
+// Threads of a workgroup, 256 / 512 / 1024: (512 x 128256 fp32, 20) 65.9 / 58.4 / 57.5, (2048 x 128256 bf16, 5) 103.6 / 100 / 110.8.
+static int logprobs_parts(int rows, int vocab, int fp32) {
+  const long long bytes = (long long)vocab * (fp32 ? 4 : 2);
+  const int parts = 256 / (rows < 1 ? 1 : rows), most = (int)(bytes / 16384);
+  if (bytes <= 192 * 1024 || parts < 4) return 1;
+  return parts < most ? parts : most;
 }
 size_t pc_logprobs_ws_bytes(int rows, int vocab, int n_top) {
-  const size_t n = (size_t)rows * logprobs_parts(rows, vocab);
+  const size_t n = (size_t)rows * logprobs_parts(rows, vocab, 1);        // (of either type: 32 bits have as many parts or more)
   return pc_align_up(n * sizeof(LogSum), 256) + pc_align_up(n * n_top * sizeof(top_key), 256) + 256;
 }
 
@@ -488,7 +495,7 @@ static int launch(const LogprobsArgs& a, hipStream_t st) {
 int pc_launch_logprobs(const PcLogprobs& c, void* ws, hipStream_t st) {
   LogprobsArgs a;
   a.c = c;
-  a.parts = logprobs_parts(c.rows, c.vocab);
+  a.parts = logprobs_parts(c.rows, c.vocab, c.fp32);
   a.parts_div = pc_div_by(a.parts);
   a.sums = (LogSum*)ws;
   a.tops = (top_key*)((char*)ws + pc_align_up((size_t)c.rows * a.parts * sizeof(LogSum), 256));

@@ -62,7 +62,7 @@ struct PcTreeCall {
   uint16_t* out;           // [B, n, H_q, D]
   float* lse;              // [B, H_q, n] or nullptr
 };
-struct PcTreePlan { int rows, tiles, shares; };      // query rows a workgroup, tiles of them a KV head, cuts of the batch's keys
+struct PcTreePlan { int rows, tiles, shares; };      // query rows a workgroup, tiles of them a KV head, cuts of the batch's keys (0: one launch)
 PcTreePlan pc_tree_plan(const PcTreeCall& c);
 bool pc_tree_fits(const PcTreeCall& c, const PcTreePlan& p);
 size_t pc_tree_ws_bytes(const PcTreeCall& c, const PcTreePlan& p);

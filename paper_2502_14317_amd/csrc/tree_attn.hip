@@ -33,7 +33,7 @@
 struct TreeArgs {
   PcTreeCall c;
   PcRope rope;
-  int group, n_tiles, n_shares, per_xcd, extra;
+  int group, n_tiles, n_shares, n_groups, per_xcd, extra;   // n_shares 0: sequences are not cut; n_groups: shares or sequences, times heads
   PcDiv group_div, tiles_div, heads_div;
   float scale_log2;
   float* part_o;           // [n_shares + B][H_kv][n group][D]
@@ -312,6 +312,12 @@ __device__ __forceinline__ void tree_query_rows(const TreeArgs& a, const TreePie
   }
 }
 
+// Place of a query row's result: [B, n, H_q]; and of its logsumexp: [B, H_q, n]
+struct TreeOut { long long row, lse; };
+__device__ __forceinline__ TreeOut tree_out(const TreeArgs& a, const TreePiece& x, int r) {
+  const int t = pc_div(x.row0 + r, a.group_div), h = x.g * a.group + x.row0 + r - t * a.group;
+  return {((long long)x.b * a.c.n + t) * a.c.n_q_heads + h, ((long long)x.b * a.c.n_q_heads + h) * a.c.n + t};
+}
 __device__ __forceinline__ long long tree_part_row(const TreeArgs& a, const TreePiece& x, int place, int r) {
   return ((long long)place * a.c.n_kv_heads + x.g) * (a.c.n * a.group) + x.row0 + r;
 }
@@ -342,6 +348,13 @@ __device__ __forceinline__ void tree_piece(const TreeArgs& a, const TreePiece& x
     sum.clear();
 #pragma unroll
     for (int w = 0; w < TREE_WAVES; ++w) sum.add(sm.few.m[w][r], sm.few.l[w][r], *(const floatx4*)&sm.few.o[w][r][d4]);
+    if (a.n_shares == 0) {                                   // the whole sequence's
+      const TreeOut to = tree_out(a, x, r);
+      const floatx4 y = sum.mean();
+      *(uint2*)(a.c.out + to.row * D + d4) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+      if (a.c.lse && d4 == 0) a.c.lse[to.lse] = sum.lse();
+      continue;
+    }
     const long long row = tree_part_row(a, x, place, r);
     *(floatx4*)(a.part_o + row * D + d4) = sum.mean();
     if (d4 == 0) a.part_lse[row] = sum.lse();
@@ -629,16 +642,24 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
     const float l = pc_rows_sum(c.l[nc]);
     const int r = 16 * (NC * wave + nc) + c16;
     if (r >= x.n_here) continue;
-    const long long row = tree_part_row(a, x, place, r);
+    const bool whole = a.n_shares == 0;
+    const TreeOut to = tree_out(a, x, r);
+    const long long row = whole ? 0 : tree_part_row(a, x, place, r);
     const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
     for (int u = 0; u < VE; ++u) {                                   // four values of the row at a time
       floatx4 y;
 #pragma unroll
       for (int w = 0; w < 4; ++w) y[w] = l == 0.f ? 0.f : (Q8 ? c.o[nc][u % (VE / 4) * 4 + w][u / (VE / 4)] : c.o[nc][u][w]) * inv;
-      *(floatx4*)(a.part_o + row * D + (Q8 ? VE * (4 * kk + u / (VE / 4)) + u % (VE / 4) * 4 : 16 * u + 4 * kk)) = y;
+      const int d = Q8 ? VE * (4 * kk + u / (VE / 4)) + u % (VE / 4) * 4 : 16 * u + 4 * kk;
+      if (whole) *(uint2*)(a.c.out + to.row * D + d) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
+      else *(floatx4*)(a.part_o + row * D + d) = y;
     }
-    if (kk == 0) a.part_lse[row] = l == 0.f ? -INFINITY : (c.ref[nc] + log2f(l)) * SHARED_LN2;
+    if (kk == 0) {
+      const float lse = l == 0.f ? -INFINITY : (c.ref[nc] + log2f(l)) * SHARED_LN2;
+      if (!whole) a.part_lse[row] = lse;
+      else if (a.c.lse) a.c.lse[to.lse] = lse;
+    }
   }
 }
 
@@ -696,34 +717,47 @@ __global__ __launch_bounds__(TREE_THREADS, 2) void tree_rows_kernel(TreeArgs a) 
   typename Body::Lds& sm = *(typename Body::Lds*)lds;
   // an XCD (number mod 8) has an eighth of (share, head, tile), the tiles behind each other: its L2 serves the keys to them
   const int at = (int)(blockIdx.x % 8) * a.per_xcd + (int)(blockIdx.x / 8);
-  if (at >= a.n_shares * a.c.n_kv_heads * a.n_tiles) return;
+  if (at >= a.n_groups * a.n_tiles) return;
   const int sg = pc_div(at, a.tiles_div), tile = at - sg * a.n_tiles;
   const int share = pc_div(sg, a.heads_div), g = sg - share * a.c.n_kv_heads;
-  int left = tree_scan(a, share, sm.scan);
-  if (left == 0) return;
-  int b = __builtin_amdgcn_readfirstlane(sm.scan.begin[0]), off = __builtin_amdgcn_readfirstlane(sm.scan.begin[1]);
-  for (; left > 0 && b < a.c.batch; ++b, off = 0) {
-    TreeSeq s;
-    if (a.c.batch <= TREE_THREADS) s = sm.scan.seq[b];
-    else s = tree_seq(a.c, b);
-    s.rows = __builtin_amdgcn_readfirstlane(s.rows); s.len = __builtin_amdgcn_readfirstlane(s.len);
-    const int nb = tree_blocks(a.c, s);
-    if (nb == 0) continue;
-    const int take = min(left, nb + a.extra - off);
-    left -= take;
-    const int blk0 = max(off - a.extra, 0), n_blk = max(off + take - a.extra, 0) - blk0;
-    if (n_blk == 0) continue;
-    if (g == 0 && tile == 0 && threadIdx.x == 0) {
-      if (blk0 == 0) a.span[b].x = share;
-      if (blk0 + n_blk == nb) a.span[b].y = share;
-    }
+  auto piece = [&](int b, const TreeSeq& s, int blk0, int n_blk, int place) __attribute__((always_inline)) {
     TreePiece x;
     x.b = b; x.g = g; x.row0 = tile * ROWS;
     x.n_here = min(ROWS, s.rows * a.group - x.row0);
-    if (x.n_here <= 0) continue;
+    if (x.n_here <= 0) return;
     x.len = tree_there(a.c, s); x.base = s.len - s.rows;
-    if constexpr (Body::FEW) tree_piece<D, Body::NC, Q8>(a, x, blk0, n_blk, share + b, sm);
-    else tree_tile_piece<D, Body::NC, Q8>(a, x, blk0, n_blk, share + b, sm);
+    if constexpr (Body::FEW) tree_piece<D, Body::NC, Q8>(a, x, blk0, n_blk, place, sm);
+    else tree_tile_piece<D, Body::NC, Q8>(a, x, blk0, n_blk, place, sm);
+  };
+  // sequences are not cut: a workgroup has a whole one's, and its result; else a share of all of them
+  const bool whole = a.n_shares == 0;
+  int left = 1, b = share, off = 0;
+  if (!whole) {
+    left = tree_scan(a, share, sm.scan);
+    if (left == 0) return;
+    b = __builtin_amdgcn_readfirstlane(sm.scan.begin[0]); off = __builtin_amdgcn_readfirstlane(sm.scan.begin[1]);
+  }
+  for (; left > 0 && b < a.c.batch; ++b, off = 0) {
+    TreeSeq s;
+    if (!whole && a.c.batch <= TREE_THREADS) s = sm.scan.seq[b];
+    else s = tree_seq(a.c, b);
+    s.rows = __builtin_amdgcn_readfirstlane(s.rows); s.len = __builtin_amdgcn_readfirstlane(s.len);
+    const int nb = tree_blocks(a.c, s);
+    int blk0 = 0, n_blk = nb;
+    if (whole) {
+      left = 0;
+    } else {
+      if (nb == 0) continue;
+      const int take = min(left, nb + a.extra - off);
+      left -= take;
+      blk0 = max(off - a.extra, 0); n_blk = max(off + take - a.extra, 0) - blk0;
+      if (n_blk == 0) continue;
+      if (g == 0 && tile == 0 && threadIdx.x == 0) {
+        if (blk0 == 0) a.span[b].x = share;
+        if (blk0 + n_blk == nb) a.span[b].y = share;
+      }
+    }
+    piece(b, s, blk0, n_blk, share + b);
   }
 }
 
@@ -785,18 +819,27 @@ PcTreePlan pc_tree_plan(const PcTreeCall& c) {
   const int rows = c.n * (c.n_q_heads / c.n_kv_heads);
   p.rows = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128));
   p.tiles = (rows + p.rows - 1) / p.rows;
-  const long long blocks = (long long)c.batch * ((((long long)c.pages.max_pages << c.pages.shift) + 31) / 32);
+  const long long cap = (long long)c.pages.max_pages << c.pages.shift, blocks = c.batch * ((cap + 31) / 32);
+  // One launch, a workgroup a sequence (and KV head and tile), where the pages hold little for each, or workgroups are many.  us a
+  // call, cut / whole, lengths from a third of the pages' on, 8 KV heads of 128 values, sequences x query rows a KV head x places:
+  //   bf16 (2 x 4 x 512) 16.3 / 11.2   (2 x 4 x 1024) 14.3 / 15.1   (16 x 4 x 1024) 21.4 / 20.3   (64 x 4 x 2048) 66.4 / 63.6
+  //   (2 x 64 x 512) 21.4 / 20.5   (16 x 64 x 1024) 30.2 / 33.5   (64 x 64 x 2048) 89 / 75   (64 x 128 x 2048) 134 / 116   (16 x 4 x 2048) 27 / 34
+  //   8 bits (2 x 4 x 1024) 14.0 / 13.7   (16 x 4 x 2048) 21.8 / 22.0   (16 x 128 x 512) 46 / 35   (64 x 128 x 2048) 138 / 117
+  if (cap <= (rows <= 32 ? 1024 : 512) || (cap <= 2048 && (long long)c.batch * c.n_kv_heads * p.tiles >= 512)) {
+    p.shares = 0;
+    return p;
+  }
   long long shares = 512 / ((long long)c.n_kv_heads * p.tiles);
   if (shares > blocks / 8) shares = blocks / 8;
   p.shares = shares < 1 ? 1 : (int)shares;
   return p;
 }
-static long long workgroups(const PcTreeCall& c, const PcTreePlan& p) { return (long long)p.shares * c.n_kv_heads * p.tiles; }
+static long long groups(const PcTreeCall& c, const PcTreePlan& p) { return (long long)(p.shares ? p.shares : c.batch) * c.n_kv_heads; }
 bool pc_tree_fits(const PcTreeCall& c, const PcTreePlan& p) {
   const long long blocks = (((long long)c.pages.max_pages << c.pages.shift) + 31) / 32;
-  return workgroups(c, p) < (1LL << 32) / TREE_THREADS - 8 && c.batch * (blocks + TREE_EXTRA) < (1LL << 31);
+  return groups(c, p) * p.tiles < (1LL << 32) / TREE_THREADS - 8 && c.batch * (blocks + TREE_EXTRA) < (1LL << 31);
 }
-static size_t part_rows(const PcTreeCall& c, const PcTreePlan& p) { return (size_t)(p.shares + c.batch) * c.n * c.n_q_heads; }
+static size_t part_rows(const PcTreeCall& c, const PcTreePlan& p) { return p.shares ? (size_t)(p.shares + c.batch) * c.n * c.n_q_heads : 0; }
 size_t pc_tree_ws_bytes(const PcTreeCall& c, const PcTreePlan& p) {
   const size_t rows = part_rows(c, p);
   return pc_align_up(rows * c.head_dim * 4, 256) + pc_align_up(rows * 4, 256) + pc_align_up((size_t)c.batch * sizeof(int2), 256);
@@ -828,7 +871,8 @@ static int launch_all(const PcTreeCall& c, const PcTreePlan& p, void* ws, hipStr
   a.c = c;
   a.rope = pc_rope_factors(c.pos ? c.rope_base : 2.0f, c.head_dim);
   a.group = c.n_q_heads / c.n_kv_heads; a.n_tiles = p.tiles; a.n_shares = p.shares;
-  a.per_xcd = (int)((workgroups(c, p) + 7) / 8); a.extra = TREE_EXTRA;
+  a.n_groups = (int)groups(c, p);
+  a.per_xcd = (int)((groups(c, p) * p.tiles + 7) / 8); a.extra = TREE_EXTRA;
   a.group_div = pc_div_by(a.group); a.tiles_div = pc_div_by(p.tiles); a.heads_div = pc_div_by(c.n_kv_heads);
   a.scale_log2 = c.scale * SHARED_LOG2E;
   const size_t rows = part_rows(c, p);
@@ -836,7 +880,7 @@ static int launch_all(const PcTreeCall& c, const PcTreePlan& p, void* ws, hipStr
   a.part_lse = (float*)((char*)ws + pc_align_up(rows * D * 4, 256));
   a.span = (int2*)((char*)a.part_lse + pc_align_up(rows * 4, 256));
   const int rc = c.pages.k_scale ? launch_body<D, true>(a, p, st) : launch_body<D, false>(a, p, st);
-  if (rc != PC_OK) return rc;
+  if (rc != PC_OK || p.shares == 0) return rc;
   const long long n_out = (long long)c.batch * c.n * c.n_q_heads;
   PcProfScope prof(PC_KERNEL_TREE_MERGE, st);
   hipLaunchKernelGGL(tree_join_kernel<D>, dim3((unsigned)((n_out * (D / 4) + 255) / 256)), dim3(256), 0, st, a, n_out, pc_div_by(c.n_q_heads),
