@@ -442,24 +442,26 @@ def _pages_fit(c, batch, n_kv_heads, head_dim):
 
 
 def _strided(t, shape, dtype, name):
-    """The address of a tensor whose rows may lie apart, and its strides but the last (0 where there is one entry)."""
-    if not t.is_cuda or t.shape != shape or t.dtype != dtype or (t.stride(-1) != 1 and t.shape[-1] > 1):
-        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, is not {dtype} {tuple(shape)} on the GPU with "
-                         "consecutive values in a row")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is {torch.cuda.current_device()}")
-    if t.is_contiguous():
-        return t.data_ptr(), (0,) * (t.dim() - 1)
-    return t.data_ptr(), tuple(s if n > 1 else 0 for s, n in zip(t.stride()[:-1], t.shape))
+    """The address of a tensor whose rows may lie apart, and the strides in front of the last (0 where there is one entry); None
+    where it is contiguous."""
+    if t.is_cuda and t.dtype is dtype and t.shape == shape and t.get_device() == torch._C._cuda_getDevice():
+        if t.is_contiguous():
+            return t.data_ptr(), None
+        strides = t.stride()
+        if strides[-1] == 1 or shape[-1] == 1:
+            strides = strides[:-1]
+            return t.data_ptr(), tuple([s if n > 1 else 0 for s, n in zip(strides, shape)]) if 1 in shape else strides
+    raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)}, strides {t.stride()}, on {t.device}, is not {dtype} {tuple(shape)} with "
+                     "consecutive values in a row on the current GPU")
 
 
 def _flat(t, n, dtype, name):
-    """The address of a tensor of n entries, or None."""
+    """The address of a contiguous tensor of n entries, or None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n:
-        raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} is not {n} entries of {dtype}")
-    return _ptr(t)
+    if t.dtype is dtype and t.numel() == n and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device} is not {n} contiguous entries of {dtype} on the GPU")
 
 
 def _rows_ref(c):
@@ -525,15 +527,17 @@ def pc_kv_append_paged(k_new, v_new, batch, n_new, n_kv_heads, head_dim, cache, 
     """cache: from make_page_cache.  k_new, v_new [B, n_new, H_kv, D], rows anywhere (the same strides for both)."""
     _pages_fit(cache, batch, n_kv_heads, head_dim)
     k = v = None
-    strides, i32 = (0, 0, 0), torch.int32
+    x, y, z, i32 = 0, 0, 0, torch.int32
     if n_new > 0 and batch > 0:
         shape = (batch, n_new, n_kv_heads, head_dim)
         (k, strides), (v, other) = _strided(k_new, shape, torch.bfloat16, "k_new"), _strided(v_new, shape, torch.bfloat16, "v_new")
-        if strides != other or not (any(strides) or k_new.is_contiguous()):
-            strides = tuple(s if m > 1 else 0 for s, m in zip(k_new.stride(), shape[:3]))
-            if strides != tuple(s if m > 1 else 0 for s, m in zip(v_new.stride(), shape[:3])) or not any(strides):
+        if strides != other:                                                # the strides of the one that is contiguous, too
+            strides, other = ([s if m > 1 else 0 for s, m in zip(t.stride(), shape[:3])] for t in (k_new, v_new))
+        if strides is not None:
+            x, y, z = strides
+            if strides != other or not (x or y or z):
                 raise ValueError(f"k_new and v_new lie differently, or all rows at one place: strides {k_new.stride()}, {v_new.stride()}")
-    _check(lib().pc_kv_append_paged(k, v, *strides, _flat(parent, batch * n_new, i32, "parent"), _flat(n_rows, batch, i32, "n_rows"),
+    _check(lib().pc_kv_append_paged(k, v, x, y, z, _flat(parent, batch * n_new, i32, "parent"), _flat(n_rows, batch, i32, "n_rows"),
                                     _flat(pos, batch, i32, "pos"), pos0, rope_base, batch, n_new, n_kv_heads, head_dim,
                                     ctypes.byref(cache), _flat(len_in, batch, i32, "len_in"), _flat(len_out, batch, i32, "len_out"),
                                     _stream()), "pc_kv_append_paged")
@@ -549,13 +553,13 @@ def pc_tree_attn(q, cache, lens, batch, n, n_q_heads, n_kv_heads, head_dim, out,
     _pages_fit(cache, batch, n_kv_heads, head_dim)
     i32, rows = torch.int32, batch * n
     at, strides = _strided(q, (batch, n, n_q_heads, head_dim), torch.bfloat16, "q")
-    if any(strides) and strides[2] not in (0, head_dim) or not (any(strides) or q.is_contiguous()) or \
-            (n_q_heads > 1 and any(strides) and strides[2] == 0):
-        raise ValueError(f"q: the heads of a node must lie behind each other, strides {q.stride()}")
-    if any(strides) and not any(strides[:2]):                               # one node of one sequence
-        strides = (0, 0, 0)
+    x = y = 0
+    if strides is not None:
+        x, y, z = strides
+        if (z != head_dim and n_q_heads > 1) or not (x or y or batch * n == 1):
+            raise ValueError(f"q: the heads of a node must lie behind each other, rows apart, strides {q.stride()}")
     p, size = _ws(ws)
-    _check(lib().pc_tree_attn(at, *strides[:2], _flat(parent, rows, i32, "parent"), _flat(n_rows, batch, i32, "n_rows"),
+    _check(lib().pc_tree_attn(at, x, y, _flat(parent, rows, i32, "parent"), _flat(n_rows, batch, i32, "n_rows"),
                               _flat(pos, batch, i32, "pos"), pos0, rope_base, softmax_scale, ctypes.byref(cache),
                               _flat(lens, batch, i32, "lens"), batch, n, n_q_heads, n_kv_heads, head_dim,
                               _flat(out, rows * n_q_heads * head_dim, torch.bfloat16, "out"),
@@ -570,8 +574,9 @@ def pc_token_logprobs(logits, rows, vocab, tokens, n_tokens, n_top, token_logpro
     """logits [rows, vocab] bfloat16 or float32, rows anywhere."""
     if logits.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError(f"logits: {logits.dtype} is neither bfloat16 nor float32")
-    at, (stride,) = _strided(logits, (rows, vocab), logits.dtype, "logits")
-    if not logits.is_contiguous() and rows > 1 and stride < vocab:
+    at, strides = _strided(logits, (rows, vocab), logits.dtype, "logits")
+    stride = 0 if strides is None else strides[0]
+    if strides is not None and rows > 1 and stride < vocab:
         raise ValueError(f"logits: rows overlap, strides {logits.stride()}")
     i32, f32 = torch.int32, torch.float32
     p, size = _ws(ws)
