@@ -501,6 +501,7 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
     from = from + 1 == STAGES ? 0 : from + 1;
     const uint8_t* ks_rows = sm.rows[stage][0];
     const uint8_t* vs_rows = sm.rows[stage][1];
+    __builtin_amdgcn_s_setprio(1);                                   // the first product goes first (64 rows 144 -> 142 us, 128 over 8 bits 350 -> 342)
     floatx4 s[NC][1][2];
 #pragma unroll
     for (int nc = 0; nc < NC; ++nc)
@@ -523,6 +524,7 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
           for (int nc = 0; nc < NC; ++nc)
             s[nc][0][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(bf16x8*)&ka, c.q[h][nc][ks], s[nc][0][bi], 0, 0, 0);
       }
+    __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);                               // (every operand in flight at once has no registers)
     vpiece vbuf[Q8 ? 8 : 1];
     const TreeLdsScales sc[1] = {{{sm.scale[stage][0] + 4 * kk}, {sm.scale[stage][1] + 4 * kk}}};
@@ -817,9 +819,14 @@ __global__ __launch_bounds__(256) void tree_join_kernel(TreeArgs a, long long n_
 PcTreePlan pc_tree_plan(const PcTreeCall& c) {
   PcTreePlan p;
   const int rows = c.n * (c.n_q_heads / c.n_kv_heads);
-  p.rows = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128));
-  p.tiles = (rows + p.rows - 1) / p.rows;
   const long long cap = (long long)c.pages.max_pages << c.pages.shift, blocks = c.batch * ((cap + 31) / 32);
+  // 17 to 32 rows: the body of 64 keeps more of the longest rows on their way, though it leaves half of its own empty.  us a call,
+  // 32 query rows a KV head, 8 KV heads, sequences x places, body of 32 / of 64:
+  //   bf16, 128 values  (2 x 512) 16 / 20   (2 x 8192) 35 / 29   (16 x 512) 18 / 23   (16 x 2048) 40 / 32   (16 x 4096) 57 / 44   (64 x 8192) 275 / 254
+  //   bf16, 64 values   (16 x 4096) 32 / 32   (16 x 16384) 73 / 83   (64 x 8192) 128 / 150
+  const bool longest = !c.pages.k_scale && c.head_dim == 128 && cap > 1024;
+  p.rows = rows <= 16 ? 16 : (rows <= 32 && !longest ? 32 : (rows <= 64 ? 64 : 128));
+  p.tiles = (rows + p.rows - 1) / p.rows;
   // One launch, a workgroup a sequence (and KV head and tile), where the pages hold little for each, or workgroups are many.  us a
   // call, cut / whole, lengths from a third of the pages' on, 8 KV heads of 128 values, sequences x query rows a KV head x places:
   //   bf16 (2 x 4 x 512) 16.3 / 11.2   (2 x 4 x 1024) 14.3 / 15.1   (16 x 4 x 1024) 21.4 / 20.3   (64 x 4 x 2048) 66.4 / 63.6
