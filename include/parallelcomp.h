@@ -508,7 +508,7 @@ typedef struct pc_page_cache {
  *   its segments.  A row that holds an infinity or a NaN reads back as NaN from 8 bits.
  *   pos [B] int32 (device), nullable (keys arrive rotated; rope_base is not looked at)
  *   len_in [B] int32 (device), nullable (all 0; at least 0); len_out [B], nullable: len_in + n_rows, whether the rows are
- *   there or not.  They must not overlap: each of a sequence's workgroups reads len_in.
+ *   there or not.  They must not overlap (refused): each of a sequence's workgroups reads len_in.
  * B * n_new * H_kv < 2^31.  No workspace. */
 int pc_kv_append_paged(const void* k_new, const void* v_new, int64_t batch_stride, int64_t row_stride, int64_t head_stride,
                        const int32_t* parent, const int32_t* n_rows, const int32_t* pos, int32_t pos0, float rope_base,
@@ -527,8 +527,8 @@ int pc_kv_append_paged(const void* k_new, const void* v_new, int64_t batch_strid
  * Arithmetic as pc_shared_attn's: bf16 MFMA products (8-bit codes widened exactly), logits, softmax and sums in fp32,
  * probabilities (at most 1; times the row's V scale) rounded to bf16 once.  The way a sequence's rows are cut, and with
  * it the last bits of its result, depends on the lengths of the whole batch; the same call gives the same bits.
- * H_q up to 2^20, batch up to 2^20, B n H_q < 2^25, B max_pages page < 2^36.  Workspace: pc_tree_attn_workspace_bytes(...) of the same sizes: it does
- * not depend on lengths, so that a captured call stays valid as they grow. */
+ * H_q up to 2^20, batch up to 2^20, B n H_q < 2^25, B max_pages page < 2^36.  Workspace: pc_tree_attn_workspace_bytes(...) of
+ * the same sizes: it does not depend on lengths, so that a captured call stays valid as they grow. */
 int pc_tree_attn(const void* q, int64_t batch_stride, int64_t row_stride, const int32_t* parent, const int32_t* n_rows,
                  const int32_t* pos, int32_t pos0, float rope_base, float softmax_scale, const pc_page_cache* cache,
                  const int32_t* len, int32_t batch, int32_t n, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -562,8 +562,9 @@ size_t pc_token_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t n_
  *     last of them, -1 if there is none
  *   cache: rows are moved; NULL: none (n_kv_heads, head_dim, len_in and len_out are not looked at).  A layer's call each; one of
  *     them brings the lengths and positions up to date.
- *   len_in [B] int32 (device): rows with the tree's; len_out [B], nullable: base + n_kept.  They must not overlap.
- *   pos [B] int32 (device), nullable: n_kept is added in place.
+ *   len_in [B] int32 (device): rows with the tree's; len_out [B], nullable: base + n_kept.
+ *   pos [B] int32 (device), nullable: n_kept is added in place.  len_in, len_out and pos must not overlap (refused where there is a
+ *     cache), and no output an input: each of a sequence's workgroups walks its tree.
  * Rows that are not there are not moved.  n 1 .. 64, batch up to 2^20.  No workspace. */
 int pc_tree_accept(const int32_t* tokens, const int32_t* parent, const int32_t* choice, int32_t choice_stride,
                    const int32_t* n_rows, int32_t batch, int32_t n, const pc_page_cache* cache, int32_t n_kv_heads,

@@ -429,6 +429,8 @@ def make_page_cache(k, v, table, k_scale=None, v_scale=None):
             raise ValueError("scales must be float32 [n_pages, n_kv_heads, page]")
     if table.dim() != 2 or table.dtype != torch.int32:
         raise ValueError("table must be int32 [batch, max_pages]")
+    if any(t is not None and t.device != k.device for t in (v, table, k_scale, v_scale)):
+        raise ValueError("pages, scales and table must be on one device")
     c = pc_page_cache(_ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale), _ptr(table), k.shape[0], k.shape[2], table.shape[1])
     c.tensors = (k, v, table, k_scale, v_scale)
     return c
@@ -439,6 +441,8 @@ def _pages_fit(c, batch, n_kv_heads, head_dim):
     if (k.shape[1], k.shape[3]) != (n_kv_heads, head_dim) or table.shape[0] != batch:
         raise ValueError(f"pages of {tuple(k.shape)} with a table of {table.shape[0]} sequences are not those of {batch} "
                          f"sequences, {n_kv_heads} KV heads of {head_dim}")
+    if k.get_device() != torch._C._cuda_getDevice():
+        raise ValueError(f"pages on {k.device}: not the current GPU")
 
 
 def _strided(t, shape, dtype, name):
@@ -459,9 +463,9 @@ def _flat(t, n, dtype, name):
     """The address of a contiguous tensor of n entries, or None."""
     if t is None:
         return None
-    if t.dtype is dtype and t.numel() == n and t.is_cuda and t.is_contiguous():
+    if t.dtype is dtype and t.numel() == n and t.is_cuda and t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice():
         return t.data_ptr()
-    raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device} is not {n} contiguous entries of {dtype} on the GPU")
+    raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device} is not {n} contiguous entries of {dtype} on the current GPU")
 
 
 def _rows_ref(c):

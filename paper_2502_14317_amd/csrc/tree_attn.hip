@@ -19,6 +19,7 @@
 #define TREE_WAVES 4
 #define TREE_EXTRA 4              // blocks that a piece costs beside its own
 #define TREE_THREADS (TREE_WAVES * PC_WAVE)
+#define TREE_GROUPS ((1LL << 32) / TREE_THREADS - 8)       // workgroups of a launch: below 2^32 threads
 // the N newest loads of this wavefront may still be on their way
 #define TREE_WAIT_LOADS(N) __builtin_amdgcn_s_waitcnt(0x0F70 | ((N) & 15) | (((N) >> 4) << 14))
 // ... and a barrier, with LDS reads done.  (A fence would wait for every load that goes to LDS.)
@@ -832,7 +833,8 @@ PcTreePlan pc_tree_plan(const PcTreeCall& c) {
   //   bf16 (2 x 4 x 512) 16.3 / 11.2   (2 x 4 x 1024) 14.3 / 15.1   (16 x 4 x 1024) 21.4 / 20.3   (64 x 4 x 2048) 66.4 / 63.6
   //   (2 x 64 x 512) 21.4 / 20.5   (16 x 64 x 1024) 30.2 / 33.5   (64 x 64 x 2048) 89 / 75   (64 x 128 x 2048) 134 / 116   (16 x 4 x 2048) 27 / 34
   //   8 bits (2 x 4 x 1024) 14.0 / 13.7   (16 x 4 x 2048) 21.8 / 22.0   (16 x 128 x 512) 46 / 35   (64 x 128 x 2048) 138 / 117
-  if (cap <= (rows <= 32 ? 1024 : 512) || (cap <= 2048 && (long long)c.batch * c.n_kv_heads * p.tiles >= 512)) {
+  const long long groups = (long long)c.batch * c.n_kv_heads * p.tiles;
+  if ((cap <= (rows <= 32 ? 1024 : 512) || (cap <= 2048 && groups >= 512)) && groups < TREE_GROUPS) {
     p.shares = 0;
     return p;
   }
@@ -844,7 +846,7 @@ PcTreePlan pc_tree_plan(const PcTreeCall& c) {
 static long long groups(const PcTreeCall& c, const PcTreePlan& p) { return (long long)(p.shares ? p.shares : c.batch) * c.n_kv_heads; }
 bool pc_tree_fits(const PcTreeCall& c, const PcTreePlan& p) {
   const long long blocks = (((long long)c.pages.max_pages << c.pages.shift) + 31) / 32;
-  return groups(c, p) * p.tiles < (1LL << 32) / TREE_THREADS - 8 && c.batch * (blocks + TREE_EXTRA) < (1LL << 31);
+  return groups(c, p) * p.tiles < TREE_GROUPS && c.batch * (blocks + TREE_EXTRA) < (1LL << 31);
 }
 static size_t part_rows(const PcTreeCall& c, const PcTreePlan& p) { return p.shares ? (size_t)(p.shares + c.batch) * c.n * c.n_q_heads : 0; }
 size_t pc_tree_ws_bytes(const PcTreeCall& c, const PcTreePlan& p) {

@@ -447,6 +447,7 @@ class PagedTreeDecoder:
                       attended to; without a parent a chain, with one row an ordinary decoding step
       accept(tokens, choice)  the path that the target's choices follow stays, its rows move together; the next token
       release(b)      sequence b's pages are free again
+    A step that has not been accepted when a sequence is loaded or released is dropped: accept() asks for the next one.
 
     Lengths and positions live on the device.  The host keeps a bound of each sequence's rows and reads the lengths only where a
     sequence could pass the end of its pages; then it takes pages for it, and raises if there are none, before anything is
@@ -508,6 +509,7 @@ class PagedTreeDecoder:
         """Sequence b has ended."""
         if _capturing(self.len):
             raise ValueError("a sequence ends outside of graphs")
+        self.at_hand = None                                                 # (its lengths are another sequence's now)
         if self.pages[b] is None:
             return
         self.free += reversed(self.pages[b])

@@ -188,3 +188,30 @@ def test_a_captured_step_goes_on():
     assert d.len.tolist() == eager.len.tolist() == [40 + 6 * 2, 40 + 6 * 3]
     d.step(*data[0], parent=parent)                                         # an eager step reads the lengths that the replays left
     assert d.most == d.len.tolist()
+
+
+def test_a_step_behind_a_load_or_release_is_dropped():
+    """Between a step and its acceptance a sequence's lengths may not become another's."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    mk = lambda *s: torch.randn(s, generator=gen, device="cuda").to(torch.bfloat16)
+    d = PagedTreeDecoder(2, 12, 16, 4, Hq, Hkv, D, BASE, max_rows=2)
+    docs = [mk(1, Hkv, 20, D) for _ in range(3)]
+    d.load(0, docs[0], docs[0], 20)
+    d.load(1, docs[1], docs[1], 20)
+    q, k, v = mk(2, 2, Hq, D), mk(2, 2, Hkv, D), mk(2, 2, Hkv, D)
+    tokens = torch.ones((2, 2), dtype=torch.int32, device="cuda")
+    want = d.step(q, k, v).clone()
+    d.load(1, docs[2], docs[2], 33)
+    with pytest.raises(ValueError, match="no step"):
+        d.accept(tokens, tokens)
+    assert d.len.tolist() == [20, 20] and d.pos.tolist() == [20, 33]
+    out = d.step(q, k, v)
+    assert torch.equal(out[0], want[0]) and not torch.equal(out[1], want[1])
+    d.release(1)
+    with pytest.raises(ValueError, match="no step"):
+        d.accept(tokens, tokens)
+    assert d.len.tolist() == [20, 0]
+    one = torch.tensor([2, 0], dtype=torch.int32, device="cuda")
+    assert torch.equal(d.step(q, k, v, n_rows=one)[0], want[0])
+    d.accept(tokens, tokens)
+    assert d.len.tolist() == [22, 0] and d.pos.tolist() == [22, 0]

@@ -9,6 +9,7 @@ import paper_2502_14317_amd as pc
 from paper_2502_14317_amd import binding
 from paper_2502_14317_amd.layer import PagedTreeDecoder
 
+LATER = ctypes.c_void_p(260)                                                # the entry behind ONE's first
 ONE, ODD, TWO, TOP = ctypes.c_void_p(256), ctypes.c_void_p(264), ctypes.c_void_p(258), ctypes.c_void_p(255)       # never dereferenced
 OK, NULL, SHAPE, WORKSPACE = 0, -1, -2, -3
 nan, inf = float("nan"), float("inf")
@@ -45,7 +46,8 @@ NO_MEMORY = [{"pages": {x: None}} for x in ("k", "v", "table")] + [{"pages": {"k
      [{"batch": -1}, {"batch": (1 << 20) + 1}, {"n_new": -1}, {"n_kv_heads": 0}, {"n_kv_heads": 1 << 17}, {"head_dim": 96},
       {"batch": 1 << 20, "n_new": 1 << 12}, {"parent": ONE, "n_new": 65}, {"row_stride": 4}, {"head_stride": -8}, {"batch_stride": 1 << 41},
       {"pos": ONE, "rope_base": 1.0}, {"pos": ONE, "rope_base": nan}, {"k_new": ODD}, {"v_new": TWO}, {"parent": TWO}, {"n_rows": TWO},
-      {"pos": TWO}, {"len_in": TWO}, {"len_out": TWO}, {"len_in": ONE, "len_out": ONE}]),
+      {"pos": TWO}, {"len_in": TWO}, {"len_out": TWO}, {"len_in": ONE, "len_out": ONE}, {"len_in": ONE, "len_out": LATER},
+      {"len_in": LATER, "len_out": ONE}]),
     ("pc_tree_attn", ATTN, WORKSPACE, [{}, {"ws": None, "ws_bytes": 1 << 40}, {"ws": ctypes.c_void_p(128), "ws_bytes": 1 << 40},
                                        {"pages": {"k_scale": ONE, "v_scale": ONE}}, {"pos": ONE, "parent": ONE, "n_rows": ONE},
                                        {"n": 64}, {"batch_stride": 1 << 20, "row_stride": 1536}]),
@@ -72,7 +74,7 @@ NO_MEMORY = [{"pages": {x: None}} for x in ("k", "v", "table")] + [{"pages": {"k
      [{"batch": -1}, {"batch": (1 << 20) + 1}, {"n": 0}, {"n": 65}, {"choice_stride": 0}, {"batch": 3, "n_kv_heads": 0}, {"batch": 3, "head_dim": 96},
       {"batch": 1 << 20, "n_kv_heads": 64}] + [dict({x: TWO}, batch=3) for x in ("tokens", "parent", "choice", "n_rows", "len_in", "len_out", "pos",
                                                                                   "path", "n_kept", "next_token")] +
-     [{"batch": 3, "len_out": ONE}]),
+     [dict(x, batch=3) for x in ({"len_out": ONE}, {"len_out": LATER}, {"pos": ONE}, {"pos": ODD}, {"len_out": ctypes.c_void_p(512), "pos": ctypes.c_void_p(508)})]),
 ])
 def test_refusals(fn, base, want, changes):
     for change in changes:
@@ -84,6 +86,7 @@ def test_workspaces():
     need = pc.lib().pc_tree_attn_workspace_bytes
     small, wide = need(cache(), 6, 5, 8, 2, 128), need(cache(max_pages=900), 6, 5, 8, 2, 128)
     assert 0 < small <= wide and need(cache(), 6, 65, 8, 2, 128) == 0 and need(cache(page=20), 6, 5, 8, 2, 128) == 0 and need(None, 6, 5, 8, 2, 128) == 0
+    assert need(cache(max_pages=8), 1 << 20, 1, 31, 31, 128) > 0            # more sequences and heads than a launch has workgroups
     need = pc.pc_token_logprobs_workspace_bytes
     assert need(3, 100000, 20) > 0 and need(3, 10, 11) == 0 and need(-1, 10, 1) == 0
 
