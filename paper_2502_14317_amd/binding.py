@@ -187,13 +187,15 @@ def _ptr(t):
     return t.data_ptr()          # a plain integer: the argument types make it a pointer
 
 
-def _stream():
+def _stream(gpu=None):
     # the handle of torch.cuda.current_stream() without the stream object around it: a decoding step of
     # a short cache is bound by its call
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if gpu is None else gpu)
 
 
-def _ws(ws):
+def _ws(ws, gpu=None):
+    if gpu is not None and ws is not None and ws.get_device() != gpu:
+        raise ValueError(f"a workspace on {ws.device}: not the current GPU")
     return (_ptr(ws), c_size_t(ws.numel() * ws.element_size())) if ws is not None else (None, c_size_t(0))
 
 
@@ -436,19 +438,24 @@ def make_page_cache(k, v, table, k_scale=None, v_scale=None):
     return c
 
 
-def _pages_fit(c, batch, n_kv_heads, head_dim):
+def _gpu():
+    """The current GPU's number."""
+    return torch._C._cuda_getDevice()
+
+
+def _pages_fit(c, batch, n_kv_heads, head_dim, gpu):
     k, _, table = c.tensors[:3]
     if (k.shape[1], k.shape[3]) != (n_kv_heads, head_dim) or table.shape[0] != batch:
         raise ValueError(f"pages of {tuple(k.shape)} with a table of {table.shape[0]} sequences are not those of {batch} "
                          f"sequences, {n_kv_heads} KV heads of {head_dim}")
-    if k.get_device() != torch._C._cuda_getDevice():
+    if k.get_device() != gpu:
         raise ValueError(f"pages on {k.device}: not the current GPU")
 
 
-def _strided(t, shape, dtype, name):
+def _strided(t, shape, dtype, name, gpu=None):
     """The address of a tensor whose rows may lie apart, and the strides in front of the last (0 where there is one entry); None
     where it is contiguous."""
-    if t.is_cuda and t.dtype is dtype and t.shape == shape and t.get_device() == torch._C._cuda_getDevice():
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.get_device() == gpu:
         if t.is_contiguous():
             return t.data_ptr(), None
         strides = t.stride()
@@ -459,11 +466,11 @@ def _strided(t, shape, dtype, name):
                      "consecutive values in a row on the current GPU")
 
 
-def _flat(t, n, dtype, name):
+def _flat(t, n, dtype, name, gpu=None):
     """The address of a contiguous tensor of n entries, or None."""
     if t is None:
         return None
-    if t.dtype is dtype and t.numel() == n and t.is_cuda and t.is_contiguous() and t.get_device() == torch._C._cuda_getDevice():
+    if t.dtype is dtype and t.numel() == n and t.get_device() == gpu and t.is_contiguous():
         return t.data_ptr()
     raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device} is not {n} contiguous entries of {dtype} on the current GPU")
 
@@ -529,22 +536,23 @@ def pc_verify_drafts(draft, draft_prob, target_prob, u, noise, batch, n_draft, v
 def pc_kv_append_paged(k_new, v_new, batch, n_new, n_kv_heads, head_dim, cache, len_in, len_out, pos=None, pos0=0, rope_base=0.0,
                        parent=None, n_rows=None):
     """cache: from make_page_cache.  k_new, v_new [B, n_new, H_kv, D], rows anywhere (the same strides for both)."""
-    _pages_fit(cache, batch, n_kv_heads, head_dim)
+    gpu = _gpu()
+    _pages_fit(cache, batch, n_kv_heads, head_dim, gpu)
     k = v = None
     x, y, z, i32 = 0, 0, 0, torch.int32
     if n_new > 0 and batch > 0:
         shape = (batch, n_new, n_kv_heads, head_dim)
-        (k, strides), (v, other) = _strided(k_new, shape, torch.bfloat16, "k_new"), _strided(v_new, shape, torch.bfloat16, "v_new")
+        (k, strides), (v, other) = _strided(k_new, shape, torch.bfloat16, "k_new", gpu), _strided(v_new, shape, torch.bfloat16, "v_new", gpu)
         if strides != other:                                                # the strides of the one that is contiguous, too
             strides, other = ([s if m > 1 else 0 for s, m in zip(t.stride(), shape[:3])] for t in (k_new, v_new))
         if strides is not None:
             x, y, z = strides
             if strides != other or not (x or y or z):
                 raise ValueError(f"k_new and v_new lie differently, or all rows at one place: strides {k_new.stride()}, {v_new.stride()}")
-    _check(lib().pc_kv_append_paged(k, v, x, y, z, _flat(parent, batch * n_new, i32, "parent"), _flat(n_rows, batch, i32, "n_rows"),
-                                    _flat(pos, batch, i32, "pos"), pos0, rope_base, batch, n_new, n_kv_heads, head_dim,
-                                    ctypes.byref(cache), _flat(len_in, batch, i32, "len_in"), _flat(len_out, batch, i32, "len_out"),
-                                    _stream()), "pc_kv_append_paged")
+    _check(lib().pc_kv_append_paged(k, v, x, y, z, _flat(parent, batch * n_new, i32, "parent", gpu), _flat(n_rows, batch, i32, "n_rows", gpu),
+                                    _flat(pos, batch, i32, "pos", gpu), pos0, rope_base, batch, n_new, n_kv_heads, head_dim,
+                                    ctypes.byref(cache), _flat(len_in, batch, i32, "len_in", gpu), _flat(len_out, batch, i32, "len_out", gpu),
+                                    _stream(gpu)), "pc_kv_append_paged")
 
 
 def pc_tree_attn_workspace_bytes(cache, batch, n, n_q_heads, n_kv_heads, head_dim):
@@ -554,20 +562,21 @@ def pc_tree_attn_workspace_bytes(cache, batch, n, n_q_heads, n_kv_heads, head_di
 def pc_tree_attn(q, cache, lens, batch, n, n_q_heads, n_kv_heads, head_dim, out, lse_out, ws, parent=None, n_rows=None, pos=None,
                  pos0=0, rope_base=0.0, softmax_scale=0.0):
     """cache: from make_page_cache.  q [B, n, H_q, D], a node's heads behind each other."""
-    _pages_fit(cache, batch, n_kv_heads, head_dim)
+    gpu = _gpu()
+    _pages_fit(cache, batch, n_kv_heads, head_dim, gpu)
     i32, rows = torch.int32, batch * n
-    at, strides = _strided(q, (batch, n, n_q_heads, head_dim), torch.bfloat16, "q")
+    at, strides = _strided(q, (batch, n, n_q_heads, head_dim), torch.bfloat16, "q", gpu)
     x = y = 0
     if strides is not None:
         x, y, z = strides
         if (z != head_dim and n_q_heads > 1) or not (x or y or batch * n == 1):
             raise ValueError(f"q: the heads of a node must lie behind each other, rows apart, strides {q.stride()}")
-    p, size = _ws(ws)
-    _check(lib().pc_tree_attn(at, x, y, _flat(parent, rows, i32, "parent"), _flat(n_rows, batch, i32, "n_rows"),
-                              _flat(pos, batch, i32, "pos"), pos0, rope_base, softmax_scale, ctypes.byref(cache),
-                              _flat(lens, batch, i32, "lens"), batch, n, n_q_heads, n_kv_heads, head_dim,
-                              _flat(out, rows * n_q_heads * head_dim, torch.bfloat16, "out"),
-                              _flat(lse_out, rows * n_q_heads, torch.float32, "lse_out"), p, size, _stream()), "pc_tree_attn")
+    p, size = _ws(ws, gpu)
+    _check(lib().pc_tree_attn(at, x, y, _flat(parent, rows, i32, "parent", gpu), _flat(n_rows, batch, i32, "n_rows", gpu),
+                              _flat(pos, batch, i32, "pos", gpu), pos0, rope_base, softmax_scale, ctypes.byref(cache),
+                              _flat(lens, batch, i32, "lens", gpu), batch, n, n_q_heads, n_kv_heads, head_dim,
+                              _flat(out, rows * n_q_heads * head_dim, torch.bfloat16, "out", gpu),
+                              _flat(lse_out, rows * n_q_heads, torch.float32, "lse_out", gpu), p, size, _stream(gpu)), "pc_tree_attn")
 
 
 def pc_token_logprobs_workspace_bytes(rows, vocab, n_top):
@@ -578,30 +587,31 @@ def pc_token_logprobs(logits, rows, vocab, tokens, n_tokens, n_top, token_logpro
     """logits [rows, vocab] bfloat16 or float32, rows anywhere."""
     if logits.dtype not in (torch.bfloat16, torch.float32):
         raise ValueError(f"logits: {logits.dtype} is neither bfloat16 nor float32")
-    at, strides = _strided(logits, (rows, vocab), logits.dtype, "logits")
+    gpu = _gpu()
+    at, strides = _strided(logits, (rows, vocab), logits.dtype, "logits", gpu)
     stride = 0 if strides is None else strides[0]
     if strides is not None and rows > 1 and stride < vocab:
         raise ValueError(f"logits: rows overlap, strides {logits.stride()}")
     i32, f32 = torch.int32, torch.float32
-    p, size = _ws(ws)
-    _check(lib().pc_token_logprobs(at, int(logits.dtype == f32), stride, _flat(tokens, rows * n_tokens, i32, "tokens"), n_tokens,
-                                   n_top, rows, vocab, _flat(token_logprob, rows * n_tokens, f32, "token_logprob"),
-                                   _flat(entropy, rows, f32, "entropy"), _flat(top_idx, rows * n_top, i32, "top_idx"),
-                                   _flat(top_logprob, rows * n_top, f32, "top_logprob"), p, size, _stream()), "pc_token_logprobs")
+    p, size = _ws(ws, gpu)
+    _check(lib().pc_token_logprobs(at, int(logits.dtype == f32), stride, _flat(tokens, rows * n_tokens, i32, "tokens", gpu), n_tokens,
+                                   n_top, rows, vocab, _flat(token_logprob, rows * n_tokens, f32, "token_logprob", gpu),
+                                   _flat(entropy, rows, f32, "entropy", gpu), _flat(top_idx, rows * n_top, i32, "top_idx", gpu),
+                                   _flat(top_logprob, rows * n_top, f32, "top_logprob", gpu), p, size, _stream(gpu)), "pc_token_logprobs")
 
 
 def pc_tree_accept(tokens, parent, choice, batch, n, path, n_kept, next_token, choice_stride=1, cache=None, n_kv_heads=0, head_dim=0,
                    len_in=None, len_out=None, pos=None, n_rows=None):
     """cache: from make_page_cache, or None (nothing moves).  choice: a node every choice_stride entries."""
-    i32, rows = torch.int32, batch * n
+    i32, rows, gpu = torch.int32, batch * n, _gpu()
     if cache is not None:
-        _pages_fit(cache, batch, n_kv_heads, head_dim)
-    one = lambda t, name: _flat(t, batch, i32, name)
-    _check(lib().pc_tree_accept(_flat(tokens, rows, i32, "tokens"), _flat(parent, rows, i32, "parent"),
-                                _flat(choice, rows * choice_stride, i32, "choice"), choice_stride, one(n_rows, "n_rows"), batch, n,
+        _pages_fit(cache, batch, n_kv_heads, head_dim, gpu)
+    one = lambda t, name: _flat(t, batch, i32, name, gpu)
+    _check(lib().pc_tree_accept(_flat(tokens, rows, i32, "tokens", gpu), _flat(parent, rows, i32, "parent", gpu),
+                                _flat(choice, rows * choice_stride, i32, "choice", gpu), choice_stride, one(n_rows, "n_rows"), batch, n,
                                 None if cache is None else ctypes.byref(cache), n_kv_heads, head_dim, one(len_in, "len_in"),
-                                one(len_out, "len_out"), one(pos, "pos"), _flat(path, rows, i32, "path"), one(n_kept, "n_kept"),
-                                one(next_token, "next_token"), _stream()), "pc_tree_accept")
+                                one(len_out, "len_out"), one(pos, "pos"), _flat(path, rows, i32, "path", gpu), one(n_kept, "n_kept"),
+                                one(next_token, "next_token"), _stream(gpu)), "pc_tree_accept")
 
 
 def pc_profile_begin(kernel=None):

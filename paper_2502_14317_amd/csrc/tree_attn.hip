@@ -390,7 +390,8 @@ struct TreeLdsScales {
   } k, v;
 };
 
-template <int D, int NC, bool Q8>
+// PARTS: bf16 parts of a query (1: they arrive rotated)
+template <int D, int NC, bool Q8, int PARTS>
 __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePiece& x, int blk0, int n_blk, int place,
                                                 typename TreeTiles<D, Q8>::Lds& sm) {
   typedef TreeTiles<D, Q8> Tiles;
@@ -475,16 +476,19 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
 #pragma unroll
     for (int ks = 0; ks < KSTEPS / 2; ++ks) {
       double theta[8];
-      if (a.c.pos) {
+      if constexpr (PARTS == 2) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) theta[e] = pc_rope_theta(a.rope, 32 * ks + 8 * kk + e);
       }
 #pragma unroll
       for (int nc = 0; nc < NC; ++nc) {
-        u32x4 u = q[nc][ks], v = q[nc][ks + KSTEPS / 2], ul = {0, 0, 0, 0}, vl = {0, 0, 0, 0};
-        if (a.c.pos) tree_turn(u, v, ul, vl, first + (__popcll(tree_above_of(mine, node_of(nc, c16))) - 1), theta);
+        u32x4 u = q[nc][ks], v = q[nc][ks + KSTEPS / 2];
+        if constexpr (PARTS == 2) {
+          u32x4 ul, vl;
+          tree_turn(u, v, ul, vl, first + (__popcll(tree_above_of(mine, node_of(nc, c16))) - 1), theta);
+          c.q[1][nc][ks] = *(bf16x8*)&ul; c.q[1][nc][ks + KSTEPS / 2] = *(bf16x8*)&vl;
+        }
         c.q[0][nc][ks] = *(bf16x8*)&u; c.q[0][nc][ks + KSTEPS / 2] = *(bf16x8*)&v;
-        c.q[1][nc][ks] = *(bf16x8*)&ul; c.q[1][nc][ks + KSTEPS / 2] = *(bf16x8*)&vl;
       }
     }
   }
@@ -520,7 +524,7 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
           ka = *(const u32x4*)(ks_rows + (k_at ^ (64 * ks)) + 16 * bi * RB);
         }
 #pragma unroll
-        for (int h = 1; h >= 0; --h)
+        for (int h = PARTS - 1; h >= 0; --h)
 #pragma unroll
           for (int nc = 0; nc < NC; ++nc)
             s[nc][0][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(bf16x8*)&ka, c.q[h][nc][ks], s[nc][0][bi], 0, 0, 0);
@@ -713,7 +717,7 @@ struct TreeBody {
   static constexpr int NC = FEW ? ROWS / 16 : ROWS / 64;
   typedef typename std::conditional<FEW, TreeLds<D, FEW ? NC : 1>, typename TreeTiles<D, Q8>::Lds>::type Lds;
 };
-template <int D, int ROWS, bool Q8>
+template <int D, int ROWS, bool Q8, int PARTS>
 __global__ __launch_bounds__(TREE_THREADS, 2) void tree_rows_kernel(TreeArgs a) {
   typedef TreeBody<D, ROWS, Q8> Body;
   extern __shared__ __align__(16) unsigned char lds[];
@@ -730,7 +734,7 @@ __global__ __launch_bounds__(TREE_THREADS, 2) void tree_rows_kernel(TreeArgs a) 
     if (x.n_here <= 0) return;
     x.len = tree_there(a.c, s); x.base = s.len - s.rows;
     if constexpr (Body::FEW) tree_piece<D, Body::NC, Q8>(a, x, blk0, n_blk, place, sm);
-    else tree_tile_piece<D, Body::NC, Q8>(a, x, blk0, n_blk, place, sm);
+    else tree_tile_piece<D, Body::NC, Q8, PARTS>(a, x, blk0, n_blk, place, sm);
   };
   // sequences are not cut: a workgroup has a whole one's, and its result; else a share of all of them
   const bool whole = a.n_shares == 0;
@@ -854,25 +858,23 @@ size_t pc_tree_ws_bytes(const PcTreeCall& c, const PcTreePlan& p) {
   return pc_align_up(rows * c.head_dim * 4, 256) + pc_align_up(rows * 4, 256) + pc_align_up((size_t)c.batch * sizeof(int2), 256);
 }
 
-template <int D, int ROWS, bool Q8>
+template <int D, int ROWS, bool Q8, int PARTS>
 static int launch_rows(const TreeArgs& a, hipStream_t st) {
   static std::atomic<uint64_t> raised{0};
   constexpr int LDS = sizeof(typename TreeBody<D, ROWS, Q8>::Lds);
-  const int rc = pc_raise_dynamic_lds((const void*)tree_rows_kernel<D, ROWS, Q8>, LDS, raised);
+  const int rc = pc_raise_dynamic_lds((const void*)tree_rows_kernel<D, ROWS, Q8, PARTS>, LDS, raised);
   if (rc != PC_OK) return rc;
   PcProfScope prof(PC_KERNEL_TREE_ATTN, st);
-  hipLaunchKernelGGL((tree_rows_kernel<D, ROWS, Q8>), dim3((unsigned)(8 * a.per_xcd)), dim3(TREE_THREADS), LDS, st, a);
+  hipLaunchKernelGGL((tree_rows_kernel<D, ROWS, Q8, PARTS>), dim3((unsigned)(8 * a.per_xcd)), dim3(TREE_THREADS), LDS, st, a);
   PC_LAUNCH_CHECK();
   return PC_OK;
 }
 template <int D, bool Q8>
 static int launch_body(const TreeArgs& a, const PcTreePlan& p, hipStream_t st) {
-  switch (p.rows) {
-    case 16: return launch_rows<D, 16, Q8>(a, st);
-    case 32: return launch_rows<D, 32, Q8>(a, st);
-    case 64: return launch_rows<D, 64, Q8>(a, st);
-    default: return launch_rows<D, 128, Q8>(a, st);
-  }
+  if (p.rows == 16) return launch_rows<D, 16, Q8, 2>(a, st);
+  if (p.rows == 32) return launch_rows<D, 32, Q8, 2>(a, st);
+  if (p.rows == 64) return a.c.pos ? launch_rows<D, 64, Q8, 2>(a, st) : launch_rows<D, 64, Q8, 1>(a, st);
+  return a.c.pos ? launch_rows<D, 128, Q8, 2>(a, st) : launch_rows<D, 128, Q8, 1>(a, st);
 }
 template <int D>
 static int launch_all(const PcTreeCall& c, const PcTreePlan& p, void* ws, hipStream_t st) {

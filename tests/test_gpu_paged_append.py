@@ -145,3 +145,13 @@ def test_graph_and_stream():
         torch.cuda.synchronize()
         for x in names:
             assert torch.equal(c[x].view(torch.uint8), want[x].view(torch.uint8)), x
+
+
+def test_tensors_of_another_gpu_are_refused():
+    """(One GPU is enough: what stands for the current one's number is another.)"""
+    k = torch.zeros((3, 1, 16, 64), dtype=torch.bfloat16, device="cuda")
+    cache = pc.make_page_cache(k, k.clone(), torch.zeros((2, 1), dtype=torch.int32, device="cuda"))
+    for refused in (lambda: pc.binding._pages_fit(cache, 2, 1, 64, 7), lambda: pc.binding._flat(cache.tensors[2], 2, torch.int32, "table", 7),
+                    lambda: pc.binding._strided(k, k.shape, torch.bfloat16, "k", 7), lambda: pc.binding._ws(k, 7)):
+        with pytest.raises(ValueError, match="current GPU"):
+            refused()
