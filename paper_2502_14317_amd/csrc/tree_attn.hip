@@ -6,10 +6,16 @@
 // The rows (node, head of the group) of a sequence and KV head are the columns of S^T = K Q^T.  A node's ancestors are the
 // bits of one 64-bit word, which a wavefront finds with six exchanges (a node a lane) and a lane keeps for its columns: the
 // mask of a tree costs a shift where a block holds rows of it, and nothing elsewhere.
-// The keys of all sequences, laid end to end in blocks of 32, are cut into equal shares, a workgroup each for a KV head and a
+// Cut: the keys of all sequences, laid end to end in blocks of 32, are cut into equal shares, a workgroup each for a KV head and a
 // tile of query rows: so a batch of very unequal lengths keeps every CU busy, whatever the table's width.  A share is a
 // piece of one sequence or of several; each piece leaves a partial (o, lse) a row at place share + sequence (both
-// only grow along the keys, so a place is taken once), and tree_join_kernel joins a sequence's.
+// only grow along the keys, so a place is taken once), and tree_join_kernel joins a sequence's.  Where there is little for a
+// sequence a workgroup takes a whole one, in one launch (pc_tree_plan).
+// Bodies: up to 32 rows a wavefront takes a part of the keys, straight into registers; more rows share keys in LDS.
+// Bound (4 D R flops against 4 D bytes a key for R query rows a KV head, 2 D + 8 in 8 bits): memory up to 64 rows, 32 sequences of
+// 8300 rows on average, 4 query rows a KV head, 8 KV heads of 128 values 167 us = 6.5 TB/s; 16 sequences of 11500 rows, 64 query
+// rows 139 us = 5.4 TB/s; with 128 rows, 8 sequences of 46000 rows in 8 bits 342 us = 0.57 PFLOP/s, 0.85 with the products of the
+// rotated queries' second parts: MFMAs busy 36 %, vector instructions 43 %, largely one after the other.
 #include <type_traits>
 #include "decode_core.h"
 #include "paged.h"
@@ -17,7 +23,8 @@
 #include "serve.h"
 
 #define TREE_WAVES 4
-#define TREE_EXTRA 4              // blocks that a piece costs beside its own
+// Blocks that a piece costs beside its own (0 / 4 / 8: 16 trees of 16 nodes 147 / 142 / 142 us, 8 of 32 over 8 bits 482 / 456 / 458)
+#define TREE_EXTRA 4
 #define TREE_THREADS (TREE_WAVES * PC_WAVE)
 #define TREE_GROUPS ((1LL << 32) / TREE_THREADS - 8)       // workgroups of a launch: below 2^32 threads
 // the N newest loads of this wavefront may still be on their way
@@ -85,9 +92,10 @@ struct TreeBlock {
   int keys[2];             // that are there
 };
 
-// A wavefront's window of the table: 64 entries from `first` on, and the 64 behind them, which are on their way
+// A wavefront's window of the table: 64 entries from `first` on.  The next 64 are waited for where they are asked for: a copy of
+// registers that are still on their way would have every block wait for all that the wavefront has asked for.
 struct TreeTable {
-  int here, next, first;
+  int here, first;
   __device__ __forceinline__ int entries(const TreeArgs& a, const TreePiece& x, int at) const {
     const int i = min(at + (int)(threadIdx.x % PC_WAVE), a.c.pages.max_pages - 1);
     return a.c.pages.table[(long long)x.b * a.c.pages.max_pages + i];
@@ -95,7 +103,6 @@ struct TreeTable {
   __device__ __forceinline__ void begin(const TreeArgs& a, const TreePiece& x, int at) {
     first = at;
     here = entries(a, x, at);
-    next = entries(a, x, at + PC_WAVE);
   }
   // are all the pages of entries lo .. hi there?
   __device__ __forceinline__ bool all(const TreeArgs& a, const TreePiece& x, int lo, int hi) const {
@@ -110,8 +117,9 @@ struct TreeTable {
   __device__ __forceinline__ long long row(const TreeArgs& a, const TreePiece& x, int key) {
     const int at = key >> a.c.pages.shift;
     if (at >= first + PC_WAVE) {
-      here = next; first += PC_WAVE;
-      next = entries(a, x, first + PC_WAVE);
+      first += PC_WAVE;
+      here = entries(a, x, first);
+      asm volatile("" : "+v"(here));
     }
     return pc_pool_row(a.c.pages, __builtin_amdgcn_readlane(here, at - first), key, x.g, a.c.n_kv_heads);
   }
@@ -363,23 +371,36 @@ __device__ __forceinline__ void tree_piece(const TreeArgs& a, const TreePiece& x
 }
 
 // ------------------------------------------------------------------------------------------ many rows
-// Blocks of 32 keys on their way from memory straight into LDS, some 64 KB of them, each read there by all four wavefronts, which
-// have 16 NC query rows each.  A row is PPR pieces of 16 bytes, piece p of row r in place p ^ swizzle(r): so the
-// matrix operands (16 rows at once, or four whole ones) come without bank conflicts, and a load instruction brings whole rows.
+// Blocks of 32 keys on their way from memory straight into LDS, 32 to 56 KB of them, each read there by all four wavefronts, which
+// have 16 NC query rows each.  8 bits: the workgroup widens a block once, a block ahead of the products (each wavefront for itself,
+// with 48 conversions and 16 permutations more a block: 128 rows 113 us instead of 110, rows of 64 values 104 instead of 102, 64 rows of
+// 128 values 150 instead of 154).  A row of 16 bits is PPR
+// pieces of 16 bytes, piece p of row r in place p ^ swizzle(r): so the matrix operands (16 rows at once, or four whole ones) come
+// without bank conflicts, and a load instruction brings whole rows.
 // (Keys straight into registers, two wavefronts to a key, keep half as many bytes on their way: 16 sequences of 11000 rows, 64
-// query rows a KV head, 188 us.)
+// query rows a KV head, 188 us instead of 140.  32 rows a wavefront, two blocks at a time: 1 to 10 us slower.)
 template <int D, bool Q8>
 struct TreeTiles {
-  static constexpr int RB = D * (Q8 ? 1 : 2), PPR = RB / 16;        // bytes, pieces of a row
-  static constexpr int STAGES = RB == 256 ? 4 : 8;
+  static constexpr int RB = D * (Q8 ? 1 : 2), WB = D * 2, PPR = WB / 16;        // bytes of a row as it comes, as it is used; pieces
+  static constexpr int STAGES = Q8 ? (D == 128 ? 5 : 8) : (D == 128 ? 4 : 8);
+  static constexpr int LAG = Q8 ? STAGES : STAGES - 1;              // blocks issued ahead of the one at hand
   static constexpr int LOADS = RB / 64 + (Q8 ? 1 : 0);              // of a wavefront, a block
-  struct Lds {
+  struct Narrow {
     uint8_t rows[STAGES][2][32 * RB];                               // [keys, values]
     float scale[STAGES][2][32];
+  };
+  struct Wide {
+    uint8_t rows[2][2][32 * WB];
+    float scale[2][2][32];
+  };
+  struct Nothing {};
+  struct Lds {
+    Narrow in;
+    typename std::conditional<Q8, Wide, Nothing>::type wide;
     unsigned long long above[PC_TREE_NODES];
     TreeScanLds scan;
   };
-  __device__ __forceinline__ static int swizzle(int row) { return PPR == 4 ? row >> 1 & 3 : row & (PPR - 1); }
+  __device__ __forceinline__ static int swizzle(int row) { return row & (PPR - 1); }
 };
 
 // A block's scales, read where they are used
@@ -395,8 +416,7 @@ template <int D, int NC, bool Q8, int PARTS>
 __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePiece& x, int blk0, int n_blk, int place,
                                                 typename TreeTiles<D, Q8>::Lds& sm) {
   typedef TreeTiles<D, Q8> Tiles;
-  constexpr int KSTEPS = D / 32, VE = D / 16, RB = Tiles::RB, PPR = Tiles::PPR, STAGES = Tiles::STAGES, AHEAD = STAGES - 1;
-  typedef uint32_t vpiece __attribute__((ext_vector_type(VE * (Q8 ? 1 : 2) / 4)));
+  constexpr int KSTEPS = D / 32, VE = D / 16, RB = Tiles::RB, WB = Tiles::WB, STAGES = Tiles::STAGES, LAG = Tiles::LAG;
   typedef __attribute__((address_space(3))) void* lptr_t;
   const int lane = tree_own(threadIdx.x % PC_WAVE), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / PC_WAVE);
   const int kk = lane / 16, c16 = lane % 16;
@@ -421,7 +441,7 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
   const int first_pos = a.c.pos ? a.c.pos[x.b] : 0;
   const unsigned long long mine = pc_tree_above(a.c.parent, x.b, a.c.n, lane);
   // Waited for in front of the loads to LDS: behind those the compiler, which does not count them through the loop, waits for too many
-  asm volatile("" : "+v"(tab.here), "+v"(tab.next));
+  asm volatile("" : "+v"(tab.here));
 #pragma unroll
   for (int nc = 0; nc < NC; ++nc)
 #pragma unroll
@@ -430,9 +450,9 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
   // ---- the blocks' loads.  Rows of 128 bytes or more: wavefront w brings rows 8 w .. of keys and values; shorter ones: half w % 2 of
   // the keys (w < 2) or values.  Rows that are not there are out of the descriptor: zeros.
   const int my_half = RB >= 128 ? wave / 2 : wave % 2, row0 = RB >= 128 ? 8 * wave : 16 * (wave % 2);      // (of the block)
-  const int at_row = row0 % 16 + lane / PPR;                         // of the half
-  const int off = at_row * RB + 16 * (lane % PPR ^ Tiles::swizzle(at_row));
-  int to = 0, from = 0;                                              // the next block's stage, the one at hand's
+  const int at_row = row0 % 16 + lane / (RB / 16);                         // of the half
+  const int off = at_row * RB + 16 * (Q8 ? lane % (RB / 16) : lane % (RB / 16) ^ Tiles::swizzle(at_row));
+  int to = 0, from = 0;                                              // the next block's stage; the one at hand's, 8 bits: that one's to widen
   uint32_t there = 0;                                                // two bits a block: are the halves' pages there
   auto issue = [&](int blk) __attribute__((always_inline)) {
     long long row[2];
@@ -453,21 +473,21 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
       const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)(kv ? a.c.pages.v : a.c.pages.k) + at * RB), 0, keys * RB, 0x00020000);
 #pragma unroll
       for (int i = 0; i < (RB == 256 ? 2 : 1); ++i)                  // (rows 4 further on: another bit of the swizzle)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(sm.rows[stage][kv] + (row0 + 4 * i) * RB), 16, off ^ (64 * i), 4 * i * RB, 0, NC == 1 ? PC_BUF_NT : 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(sm.in.rows[stage][kv] + (row0 + 4 * i) * RB), 16, off ^ (64 * i), 4 * i * RB, 0, NC == 1 ? PC_BUF_NT : 0);
     }
     if constexpr (Q8) {                                              // 16 scales: of the keys (even wavefronts) or values of half w / 2
       const long long rs = wave / 2 ? row[1] : row[0];
       const int n = rs < 0 ? 0 : min(16, x.len - 32 * blk - 16 * (wave / 2));
       const float* scales = wave % 2 ? a.c.pages.v_scale : a.c.pages.k_scale;
       const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(scales + (rs < 0 ? 0 : rs)), 0, n * 4, 0x00020000);
-      if (lane < 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(sm.scale[stage][wave % 2] + 16 * (wave / 2)), 4, lane * 4, 0, 0, 0);
+      if (lane < 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(sm.in.scale[stage][wave % 2] + 16 * (wave / 2)), 4, lane * 4, 0, 0, 0);
     }
   };
   __builtin_amdgcn_sched_barrier(0);
   __syncthreads();                                                   // (the piece before this one is done with LDS)
   if (wave == 0) sm.above[lane] = mine;
 #pragma unroll 1
-  for (int i = 0; i < AHEAD; ++i) issue(blk0 + i);
+  for (int i = 0; i < LAG; ++i) issue(blk0 + i);
   __builtin_amdgcn_sched_barrier(0);
 
   // ---- meanwhile the rotation
@@ -493,65 +513,87 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
     }
   }
 
-  const int k_at = Q8 ? c16 * RB + 16 * ((kk / 2) ^ Tiles::swizzle(c16)) + 8 * (kk % 2) : c16 * RB + 16 * (kk ^ Tiles::swizzle(c16));
-  // 8 bits: a lane's VE values of its 8 keys (rows 4 kk + i, 16 + 4 kk + i), operand e of V^T is value VE d + e of row d of the
-  // result.  16 bits: reads that transpose (16 lanes point at 4 rows of 16 values, 8 bytes a lane, and get a value's 4 rows): operand e
-  // is values 16 e + d.
-  const int v_byte = VE * c16;
-  const int v_at = Q8 ? 4 * kk * RB + 16 * (v_byte / 16 ^ Tiles::swizzle(4 * kk)) + v_byte % 16
-                      : (4 * kk + c16 / 4) * RB + 16 * (c16 % 4 / 2 ^ Tiles::swizzle(4 * kk + c16 / 4)) + 8 * (c16 % 2);
+  const int k_at = c16 * WB + 16 * (kk ^ Tiles::swizzle(c16));
+  // reads that transpose: 16 lanes point at 4 rows of 16 values, 8 bytes a lane, and get a value's 4 rows: operand e is values 16 e + d
+  const int v_at = (4 * kk + c16 / 4) * WB + 16 * (c16 % 4 / 2 ^ Tiles::swizzle(4 * kk + c16 / 4)) + 8 * (c16 % 2);
+  // 8 bits: a thread's 16 codes of the keys, of the values (rows of 64 values: of either), which it widens
+  constexpr int CODES = Q8 ? D / 64 : 1;
+  const int w_row = threadIdx.x % (2 * D) / (D / 16), w_piece = threadIdx.x % (D / 16), w_side = D == 64 ? threadIdx.x / 128 : 0;
+  const int w_at = w_row * WB + 16 * (2 * w_piece ^ Tiles::swizzle(w_row));
+  u32x4 codes[CODES];
+  float w_scale = 0.f;
+  auto take = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < CODES; ++i) codes[i] = *(const u32x4*)(sm.in.rows[from][w_side + i] + w_row * RB + 16 * w_piece);
+    w_scale = sm.in.scale[from][threadIdx.x / 32 % 2][threadIdx.x % 32];
+    from = from + 1 == STAGES ? 0 : from + 1;
+  };
+  auto widen = [&](int to_half) __attribute__((always_inline)) {
+    if constexpr (Q8) {
+#pragma unroll
+      for (int i = 0; i < CODES; ++i) {
+        uint8_t* at = sm.wide.rows[to_half][w_side + i];
+        *(u32x4*)(at + w_at) = u32x4{shared_widen(codes[i][0], false), shared_widen(codes[i][0], true), shared_widen(codes[i][1], false), shared_widen(codes[i][1], true)};
+        *(u32x4*)(at + (w_at ^ 16)) = u32x4{shared_widen(codes[i][2], false), shared_widen(codes[i][2], true), shared_widen(codes[i][3], false), shared_widen(codes[i][3], true)};
+      }
+      if (threadIdx.x < 64) sm.wide.scale[to_half][threadIdx.x / 32][threadIdx.x % 32] = w_scale;
+    }
+  };
+  int half = 0;                                                      // of the widened blocks, the one at hand
   auto block = [&](auto masked_tag, int blk, const bool (&in)[2]) __attribute__((always_inline)) {
     constexpr bool MASKED = decltype(masked_tag)::value;
-    const int stage = from;
-    from = from + 1 == STAGES ? 0 : from + 1;
-    const uint8_t* ks_rows = sm.rows[stage][0];
-    const uint8_t* vs_rows = sm.rows[stage][1];
+    const uint8_t *ks_rows, *vs_rows;
+    const float* scales = nullptr;
+    if constexpr (Q8) {
+      ks_rows = sm.wide.rows[half][0]; vs_rows = sm.wide.rows[half][1]; scales = sm.wide.scale[half][0] + 4 * kk;
+      take();                                                        // (the next one's)
+    } else {
+      ks_rows = sm.in.rows[from][0]; vs_rows = sm.in.rows[from][1];
+      from = from + 1 == STAGES ? 0 : from + 1;
+    }
     __builtin_amdgcn_s_setprio(1);                                   // the first product goes first (64 rows 144 -> 142 us, 128 over 8 bits 350 -> 342)
     floatx4 s[NC][1][2];
 #pragma unroll
     for (int nc = 0; nc < NC; ++nc)
 #pragma unroll
       for (int bi = 0; bi < 2; ++bi) s[nc][0][bi] = floatx4{0.f, 0.f, 0.f, 0.f};
+    u32x4 ka[2][2];                                                  // a step's and the next one's operands, which are on their way
+    auto key_operands = [&](int ks) __attribute__((always_inline)) {
 #pragma unroll
-    for (int ks = 0; ks < KSTEPS; ++ks)
+      for (int bi = 0; bi < 2; ++bi) ka[ks % 2][bi] = *(const u32x4*)(ks_rows + (k_at ^ (64 * ks)) + 16 * bi * WB);
+    };
+    key_operands(0);
 #pragma unroll
-      for (int bi = 0; bi < 2; ++bi) {
-        u32x4 ka;
-        if constexpr (Q8) {
-          const u32x2 w = *(const u32x2*)(ks_rows + (k_at ^ (32 * ks)) + 16 * bi * RB);
-          ka = u32x4{shared_widen(w[0], false), shared_widen(w[0], true), shared_widen(w[1], false), shared_widen(w[1], true)};
-        } else {
-          ka = *(const u32x4*)(ks_rows + (k_at ^ (64 * ks)) + 16 * bi * RB);
-        }
+    for (int ks = 0; ks < KSTEPS; ++ks) {
+      if (ks + 1 < KSTEPS) key_operands(ks + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int h = PARTS - 1; h >= 0; --h)
+      for (int h = PARTS - 1; h >= 0; --h)
+#pragma unroll
+        for (int bi = 0; bi < 2; ++bi)
 #pragma unroll
           for (int nc = 0; nc < NC; ++nc)
-            s[nc][0][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(bf16x8*)&ka, c.q[h][nc][ks], s[nc][0][bi], 0, 0, 0);
-      }
+            s[nc][0][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(bf16x8*)&ka[ks % 2][bi], c.q[h][nc][ks], s[nc][0][bi], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (Q8) widen(half ^ 1);
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);                               // (every operand in flight at once has no registers)
-    vpiece vbuf[Q8 ? 8 : 1];
-    const TreeLdsScales sc[1] = {{{sm.scale[stage][0] + 4 * kk}, {sm.scale[stage][1] + 4 * kk}}};
+    const TreeLdsScales sc[1] = {{{scales}, {scales + 32}}};
     u32x4 va4[4];                                                    // four operands of V^T
     auto value_operands = [&](int e0) __attribute__((always_inline)) {
-      if constexpr (Q8) {
+      // (the builtin would be taken to read what is on its way to LDS, and wait for all of it)
+      const uint32_t at = (uint32_t)(uintptr_t)(lptr_t)(vs_rows + 0);
+      const uint32_t a0 = at + (v_at ^ (32 * e0)), a1 = at + (v_at ^ (32 * (e0 + 1))), a2 = at + (v_at ^ (32 * (e0 + 2))), a3 = at + (v_at ^ (32 * (e0 + 3)));
+      u32x2 r[8];
+      asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+                   "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+                   "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+                   "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\ts_waitcnt lgkmcnt(0)"
+                   : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+                   : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "n"(16 * WB) : "memory");
 #pragma unroll
-        for (int e = 0; e < 4; ++e) va4[e] = shared_value_operand<Q8>(vbuf, e0 + e);
-      } else {
-        // (the builtin would be taken to read what is on its way to LDS, and wait for all of it)
-        const uint32_t at = (uint32_t)(uintptr_t)(lptr_t)(vs_rows + 0);
-        const uint32_t a0 = at + (v_at ^ (32 * e0)), a1 = at + (v_at ^ (32 * (e0 + 1))), a2 = at + (v_at ^ (32 * (e0 + 2))), a3 = at + (v_at ^ (32 * (e0 + 3)));
-        u32x2 r[8];
-        asm volatile("ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
-                     "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
-                     "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
-                     "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\ts_waitcnt lgkmcnt(0)"
-                     : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
-                     : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "n"(16 * RB) : "memory");
-#pragma unroll
-        for (int e = 0; e < 4; ++e) va4[e] = u32x4{r[2 * e][0], r[2 * e][1], r[2 * e + 1][0], r[2 * e + 1][1]};
-      }
+      for (int e = 0; e < 4; ++e) va4[e] = u32x4{r[2 * e][0], r[2 * e][1], r[2 * e + 1][0], r[2 * e + 1][1]};
     };
     const int rel = 32 * blk - x.base;
     unsigned long long above[NC];
@@ -569,11 +611,6 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
     u32x4 p[NC][1];
     shared_softmax<NC, 1, VE, Q8, !MASKED>(s, sc, MASKED, hidden, a.scale_log2, c.ref, c.sub, c.l, c.o, p);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (Q8) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        vbuf[i] = *(const vpiece*)(vs_rows + (v_at ^ (16 * (PPR == 4 ? i % 4 / 2 : i % 4))) + (i < 4 ? i : i + 12) * RB);
-    }
     uint32_t not_finite = 0;
 #pragma unroll
     for (int e = 0; e < VE; ++e) {
@@ -610,9 +647,8 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
           for (int e = 0; e < VE; ++e)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const int d = Q8 ? VE * (4 * tree_own(own_kk) + i) + e : 16 * e + 4 * tree_own(own_kk) + i, byte = d * (Q8 ? 1 : 2);
-              const uint8_t* at = vs_rows + key * RB + 16 * (byte / 16 ^ Tiles::swizzle(key)) + byte % 16;
-              const float v = Q8 ? ((*at & 0x7f) == 0x7f ? NAN : 0.f) : bf16_bits_to_f32(*(const uint16_t*)at);
+              const int byte = 2 * (16 * e + 4 * tree_own(own_kk) + i);
+              const float v = bf16_bits_to_f32(*(const uint16_t*)(vs_rows + key * WB + 16 * (byte / 16 ^ Tiles::swizzle(key)) + byte % 16));
               const bool bad = !(fabsf(v) < INFINITY);
 #pragma unroll
               for (int nc = 0; nc < NC; ++nc) c.o[nc][e][i] += bad && (seen[nc] >> key & 1) ? v : 0.f;
@@ -621,24 +657,29 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
       }
     }
   };
-  // Block `blk` has arrived when all but the wavefront's loads of the AHEAD - 1 blocks behind it have, and everybody says so; by then
-  // everybody has left the block in front of it, whose place the next one takes.
-  // Blocks that every column sees whole come first, in a loop of their own (none where one of the piece's pages is not there).
+  // A block has arrived when all but the wavefront's loads of those behind it have, and everybody says so; by then everybody has left
+  // the block in front of it, whose place the next one takes.  8 bits: the block behind the one at hand has, to be widened, and the one
+  // at hand is.  Blocks that every column sees whole come first, in a loop of their own (none where one of the piece's pages is not there).
   const int whole_end = all_there ? min(end, max(x.base, 0) / 32) : blk0;
   auto arrive = [&](int blk) __attribute__((always_inline)) {
-    TREE_TILE_BARRIER((AHEAD - 1) * Tiles::LOADS);
-    issue(blk + AHEAD);
+    TREE_TILE_BARRIER((LAG - (Q8 ? 2 : 1)) * Tiles::LOADS);
+    issue(blk + LAG);
     __builtin_amdgcn_sched_barrier(0);
   };
+  if constexpr (Q8) {
+    TREE_TILE_BARRIER((LAG - 1) * Tiles::LOADS);
+    take();
+    widen(half);
+  }
   int blk = blk0;
-  for (; blk < whole_end; ++blk) {
+  for (; blk < whole_end; ++blk, half ^= 1) {
     arrive(blk);
     const bool in[2] = {true, true};
     block(std::integral_constant<bool, false>{}, blk, in);
   }
-  for (; blk < end; ++blk) {
+  for (; blk < end; ++blk, half ^= 1) {
     arrive(blk);
-    const bool in[2] = {(there >> (2 * AHEAD) & 1) != 0, (there >> (2 * AHEAD) & 2) != 0};
+    const bool in[2] = {(there >> (2 * LAG) & 1) != 0, (there >> (2 * LAG) & 2) != 0};
     block(std::integral_constant<bool, true>{}, blk, in);
   }
   TREE_WAIT_LOADS(0);                                                // (nothing is on its way to LDS when the workgroup ends)
@@ -657,8 +698,8 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
     for (int u = 0; u < VE; ++u) {                                   // four values of the row at a time
       floatx4 y;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) y[w] = l == 0.f ? 0.f : (Q8 ? c.o[nc][u % (VE / 4) * 4 + w][u / (VE / 4)] : c.o[nc][u][w]) * inv;
-      const int d = Q8 ? VE * (4 * kk + u / (VE / 4)) + u % (VE / 4) * 4 : 16 * u + 4 * kk;
+      for (int w = 0; w < 4; ++w) y[w] = l == 0.f ? 0.f : c.o[nc][u][w] * inv;
+      const int d = 16 * u + 4 * kk;
       if (whole) *(uint2*)(a.c.out + to.row * D + d) = make_uint2(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]));
       else *(floatx4*)(a.part_o + row * D + d) = y;
     }
