@@ -92,13 +92,17 @@ struct TreeBlock {
   int keys[2];             // that are there
 };
 
-// A wavefront's window of the table: 64 entries from `first` on.  The next 64 are waited for where they are asked for: a copy of
-// registers that are still on their way would have every block wait for all that the wavefront has asked for.
+// A wavefront's window of the table: where the rows of 64 pages from entry `first` on begin in the pool (negative: no page).  The
+// next 64 are waited for where they are asked for: a copy of registers that are still on their way would have every block
+// wait for all that the wavefront has asked for.
 struct TreeTable {
-  int here, first;
-  __device__ __forceinline__ int entries(const TreeArgs& a, const TreePiece& x, int at) const {
+  long long here;
+  int first;
+  __device__ __forceinline__ long long entries(const TreeArgs& a, const TreePiece& x, int at) const {
     const int i = min(at + (int)(threadIdx.x % PC_WAVE), a.c.pages.max_pages - 1);
-    return a.c.pages.table[(long long)x.b * a.c.pages.max_pages + i];
+    const int page = a.c.pages.table[(long long)x.b * a.c.pages.max_pages + i];
+    const long long row = pc_pool_row(a.c.pages, page, 0, x.g, a.c.n_kv_heads);
+    return row < 0 ? -(1LL << 40) : row;
   }
   __device__ __forceinline__ void begin(const TreeArgs& a, const TreePiece& x, int at) {
     first = at;
@@ -108,12 +112,12 @@ struct TreeTable {
   __device__ __forceinline__ bool all(const TreeArgs& a, const TreePiece& x, int lo, int hi) const {
     bool there = true;
     for (int at = lo; at <= hi; at += PC_WAVE) {
-      const int page = at == lo ? here : entries(a, x, at);
-      there &= at + (int)(threadIdx.x % PC_WAVE) > hi || (uint32_t)page < (uint32_t)a.c.pages.n_pages;
+      const long long row = at == lo ? here : entries(a, x, at);
+      there &= at + (int)(threadIdx.x % PC_WAVE) > hi || row >= 0;
     }
     return __all(there);
   }
-  // the row of the pool where key `key` lies, -1 if it is not there; keys are asked for in order
+  // the row of the pool where key `key` lies, negative if it is not there; keys are asked for in order
   __device__ __forceinline__ long long row(const TreeArgs& a, const TreePiece& x, int key) {
     const int at = key >> a.c.pages.shift;
     if (at >= first + PC_WAVE) {
@@ -121,7 +125,9 @@ struct TreeTable {
       here = entries(a, x, first);
       asm volatile("" : "+v"(here));
     }
-    return pc_pool_row(a.c.pages, __builtin_amdgcn_readlane(here, at - first), key, x.g, a.c.n_kv_heads);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)here, at - first);
+    const int hi = __builtin_amdgcn_readlane((int)(here >> 32), at - first);
+    return ((long long)hi << 32 | lo) + (key & ((1 << a.c.pages.shift) - 1));
   }
 };
 
@@ -447,47 +453,49 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) asm volatile("" : "+v"(q[nc][ks]));
 
-  // ---- the blocks' loads.  Rows of 128 bytes or more: wavefront w brings rows 8 w .. of keys and values; shorter ones: half w % 2 of
-  // the keys (w < 2) or values.  Rows that are not there are out of the descriptor: zeros.
-  const int my_half = RB >= 128 ? wave / 2 : wave % 2, row0 = RB >= 128 ? 8 * wave : 16 * (wave % 2);      // (of the block)
-  const int at_row = row0 % 16 + lane / (RB / 16);                         // of the half
+  // ---- the blocks' loads: wavefront w brings half w / 2 of a block, rows 8 w .. of keys and values, or, of rows shorter than 128 bytes, all 16
+  // of the keys or values; and 16 scales of the keys or values.  Rows that are not there are out of the descriptor: zeros.
+  const int my_half = wave / 2, row0 = RB >= 128 ? 8 * wave : 16 * my_half;      // (of the block)
+  const int at_row = row0 % 16 + lane / (RB / 16);                   // of the half
   const int off = at_row * RB + 16 * (Q8 ? lane % (RB / 16) : lane % (RB / 16) ^ Tiles::swizzle(at_row));
   int to = 0, from = 0;                                              // the next block's stage; the one at hand's, 8 bits: that one's to widen
-  uint32_t there = 0;                                                // two bits a block: are the halves' pages there
-  auto issue = [&](int blk) __attribute__((always_inline)) {
-    long long row[2];
+  uint32_t there = 0;                                                // two bits a block, where pages are missing: are the halves' there
+  auto issue = [&](int blk, bool known) __attribute__((always_inline)) {          // known: that all pages are there
+    const int key = 32 * blk + 16 * my_half;
+    int keys = blk < end ? min(x.len - key, 16) : 0;
+    long long at = 0;
+    if (known || all_there) {                                        // (a wavefront needs to know of its half alone)
+      if (keys > 0) at = tab.row(a, x, key);
+    } else {
+      long long row[2];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int key = 32 * blk + 16 * h;
-      row[h] = blk < end && key < x.len ? tab.row(a, x, key) : -1;
+      for (int h = 0; h < 2; ++h) row[h] = blk < end && 32 * blk + 16 * h < x.len ? tab.row(a, x, 32 * blk + 16 * h) : -1;
+      there = there << 2 | (row[0] >= 0 ? 1u : 0u) | (row[1] >= 0 ? 2u : 0u);
+      at = my_half ? row[1] : row[0];
+      if (at < 0) at = keys = 0;
     }
-    there = there << 2 | (row[0] >= 0 ? 1u : 0u) | (row[1] >= 0 ? 2u : 0u);
+    keys = max(keys, 0);
     const int stage = to;
     to = to + 1 == STAGES ? 0 : to + 1;
-    const long long r = my_half ? row[1] : row[0];
-    const int keys = r < 0 ? 0 : min(16, x.len - 32 * blk - 16 * my_half);
-    const long long at = r < 0 ? 0 : r;
 #pragma unroll
     for (int kv = 0; kv < 2; ++kv) {
-      if (RB < 128 && kv != wave / 2) continue;
+      if (RB < 128 && kv != wave % 2) continue;
       const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)(kv ? a.c.pages.v : a.c.pages.k) + at * RB), 0, keys * RB, 0x00020000);
 #pragma unroll
       for (int i = 0; i < (RB == 256 ? 2 : 1); ++i)                  // (rows 4 further on: another bit of the swizzle)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(sm.in.rows[stage][kv] + (row0 + 4 * i) * RB), 16, off ^ (64 * i), 4 * i * RB, 0, NC == 1 ? PC_BUF_NT : 0);
     }
-    if constexpr (Q8) {                                              // 16 scales: of the keys (even wavefronts) or values of half w / 2
-      const long long rs = wave / 2 ? row[1] : row[0];
-      const int n = rs < 0 ? 0 : min(16, x.len - 32 * blk - 16 * (wave / 2));
+    if constexpr (Q8) {
       const float* scales = wave % 2 ? a.c.pages.v_scale : a.c.pages.k_scale;
-      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(scales + (rs < 0 ? 0 : rs)), 0, n * 4, 0x00020000);
-      if (lane < 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(sm.in.scale[stage][wave % 2] + 16 * (wave / 2)), 4, lane * 4, 0, 0, 0);
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)(scales + at), 0, keys * 4, 0x00020000);
+      if (lane < 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lptr_t)(sm.in.scale[stage][wave % 2] + 16 * my_half), 4, lane * 4, 0, 0, 0);
     }
   };
   __builtin_amdgcn_sched_barrier(0);
   __syncthreads();                                                   // (the piece before this one is done with LDS)
   if (wave == 0) sm.above[lane] = mine;
 #pragma unroll 1
-  for (int i = 0; i < LAG; ++i) issue(blk0 + i);
+  for (int i = 0; i < LAG; ++i) issue(blk0 + i, false);
   __builtin_amdgcn_sched_barrier(0);
 
   // ---- meanwhile the rotation
@@ -554,19 +562,24 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
       ks_rows = sm.in.rows[from][0]; vs_rows = sm.in.rows[from][1];
       from = from + 1 == STAGES ? 0 : from + 1;
     }
-    if (idle) return;
-    __builtin_amdgcn_s_setprio(1);                                   // the first product goes first (64 rows 144 -> 142 us, 128 over 8 bits 350 -> 342)
-    floatx4 s[NC][1][2];
-#pragma unroll
-    for (int nc = 0; nc < NC; ++nc)
-#pragma unroll
-      for (int bi = 0; bi < 2; ++bi) s[nc][0][bi] = floatx4{0.f, 0.f, 0.f, 0.f};
+    if (idle) {
+      issue(blk + LAG, !MASKED);
+      return;
+    }
     u32x4 ka[2][2];                                                  // a step's and the next one's operands, which are on their way
     auto key_operands = [&](int ks) __attribute__((always_inline)) {
 #pragma unroll
       for (int bi = 0; bi < 2; ++bi) ka[ks % 2][bi] = *(const u32x4*)(ks_rows + (k_at ^ (64 * ks)) + 16 * bi * WB);
     };
     key_operands(0);
+    issue(blk + LAG, !MASKED);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);                                   // the first product goes first (64 rows 144 -> 142 us, 128 over 8 bits 350 -> 342)
+    floatx4 s[NC][1][2];
+#pragma unroll
+    for (int nc = 0; nc < NC; ++nc)
+#pragma unroll
+      for (int bi = 0; bi < 2; ++bi) s[nc][0][bi] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int ks = 0; ks < KSTEPS; ++ks) {
       if (ks + 1 < KSTEPS) key_operands(ks + 1);
@@ -665,9 +678,8 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
   // the block in front of it, whose place the next one takes.  8 bits: the block behind the one at hand has, to be widened, and the one
   // at hand is.  Blocks that every column sees whole come first, in a loop of their own (none where one of the piece's pages is not there).
   const int whole_end = all_there ? min(end, max(x.base, 0) / 32) : blk0;
-  auto arrive = [&](int blk) __attribute__((always_inline)) {
+  auto arrive = [&]() __attribute__((always_inline)) {
     TREE_TILE_BARRIER((LAG - (Q8 ? 2 : 1)) * Tiles::LOADS);
-    issue(blk + LAG);
     __builtin_amdgcn_sched_barrier(0);
   };
   if constexpr (Q8) {
@@ -677,13 +689,13 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
   }
   int blk = blk0;
   for (; blk < whole_end; ++blk, half ^= 1) {
-    arrive(blk);
+    arrive();
     const bool in[2] = {true, true};
     block(std::integral_constant<bool, false>{}, blk, in);
   }
   for (; blk < end; ++blk, half ^= 1) {
-    arrive(blk);
-    const bool in[2] = {(there >> (2 * LAG) & 1) != 0, (there >> (2 * LAG) & 2) != 0};
+    arrive();
+    const bool in[2] = {all_there || (there >> (2 * LAG - 2) & 1) != 0, all_there || (there >> (2 * LAG - 2) & 2) != 0};
     block(std::integral_constant<bool, true>{}, blk, in);
   }
   TREE_WAIT_LOADS(0);                                                // (nothing is on its way to LDS when the workgroup ends)
