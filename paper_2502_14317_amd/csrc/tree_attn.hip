@@ -409,14 +409,6 @@ struct TreeTiles {
   __device__ __forceinline__ static int swizzle(int row) { return row & (PPR - 1); }
 };
 
-// A block's scales, read where they are used
-struct TreeLdsScales {
-  struct Side {
-    const float* at;
-    __device__ __forceinline__ floatx4 operator[](int bi) const { return *(const floatx4*)(at + 16 * bi); }
-  } k, v;
-};
-
 // PARTS: bf16 parts of a query (1: they arrive rotated)
 template <int D, int NC, bool Q8, int PARTS>
 __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePiece& x, int blk0, int n_blk, int place,
@@ -572,6 +564,11 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
       for (int bi = 0; bi < 2; ++bi) ka[ks % 2][bi] = *(const u32x4*)(ks_rows + (k_at ^ (64 * ks)) + 16 * bi * WB);
     };
     key_operands(0);
+    SharedScales sc[1];                                              // on their way in front of the products that they wait behind
+    if constexpr (Q8) {
+#pragma unroll
+      for (int bi = 0; bi < 2; ++bi) sc[0].k[bi] = *(const floatx4*)(scales + 16 * bi);
+    }
     issue(blk + LAG, !MASKED);
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_setprio(1);                                   // the first product goes first (64 rows 144 -> 142 us, 128 over 8 bits 350 -> 342)
@@ -593,10 +590,13 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
             s[nc][0][bi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*(bf16x8*)&ka[ks % 2][bi], c.q[h][nc][ks], s[nc][0][bi], 0, 0, 0);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (Q8) widen(half ^ 1);
+    if constexpr (Q8) {
+#pragma unroll
+      for (int bi = 0; bi < 2; ++bi) sc[0].v[bi] = *(const floatx4*)(scales + 32 + 16 * bi);
+      widen(half ^ 1);
+    }
     __builtin_amdgcn_s_setprio(0);
     __builtin_amdgcn_sched_barrier(0);                               // (every operand in flight at once has no registers)
-    const TreeLdsScales sc[1] = {{{scales}, {scales + 32}}};
     u32x4 va4[4];                                                    // four operands of V^T
     auto value_operands = [&](int e0) __attribute__((always_inline)) {
       // (the builtin would be taken to read what is on its way to LDS, and wait for all of it)
