@@ -14,8 +14,9 @@
 // Bodies: up to 32 rows a wavefront takes a part of the keys, straight into registers; more rows share keys in LDS.
 // Bound (4 D R flops against 4 D bytes a key for R query rows a KV head, 2 D + 8 in 8 bits): memory up to 64 rows, 32 sequences of
 // 8300 rows on average, 4 query rows a KV head, 8 KV heads of 128 values 167 us = 6.5 TB/s; 16 sequences of 11500 rows, 64 query
-// rows 139 us = 5.4 TB/s; with 128 rows, 8 sequences of 46000 rows in 8 bits 342 us = 0.57 PFLOP/s, 0.85 with the products of the
-// rotated queries' second parts: MFMAs busy 36 %, vector instructions 43 %, largely one after the other.
+// rows 138 us = 5.5 TB/s; with 128 rows, 8 sequences of 46000 rows in 8 bits 328 us = 0.59 PFLOP/s, 0.89 with the products of the
+// rotated queries' second parts: a block's chain of a barrier, scalar instructions, reads of LDS, products and softmax, of which
+// two wavefronts a SIMD hide a part of each other's (what was taken off the chain gained, what was taken off the counts did not).
 #include <type_traits>
 #include "decode_core.h"
 #include "paged.h"
