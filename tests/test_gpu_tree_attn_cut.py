@@ -212,3 +212,45 @@ def test_sequences_that_share_pages():
     c["table"][1:, :29] = c["table"][0, :29]                                # 464 rows, the trees' rows are their own
     out, lse, _ = call(c)
     check_attention(out, lse, c, "shared", NO)
+
+
+@pytest.mark.parametrize("gaps", [False, True], ids=["whole", "gaps"])
+@pytest.mark.parametrize("n,Hq,Hkv,D,fmt", [(1, 512, 512, 64, "bf16"), (1, 512, 512, 128, "row8"), (24, 512, 512, 64, "row8"), (24, 256, 256, 64, "bf16"),
+                                            (24, 256, 256, 128, "bf16"), (64, 256, 256, 64, "bf16"), (64, 256, 256, 128, "row8"),
+                                            (64, 256, 128, 128, "bf16"), (64, 256, 128, 64, "row8")], ids=str)
+def test_pieces_of_many_pages(n, Hq, Hkv, D, fmt, gaps):
+    """A workgroup's piece of a sequence that spans several windows of 64 table entries: pages of 16 rows give what the same rows in
+    pages of 256 do, bit for bit."""
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    B, big, lens = 2, 256, [4500 + n, 3111 + n]
+    P = 2 * 20
+    shape, c = (P, Hkv, big), {"B": B, "n": n, "Hq": Hq, "Hkv": Hkv, "D": D, "pos0": 3, "base": 1e4, "n_rows": None}
+    for name in "kv":
+        if fmt == "bf16":
+            c[name], c[name + "_scale"] = torch.randn((*shape, D), generator=gen, device="cuda", dtype=torch.bfloat16), None
+        else:
+            c[name] = torch.randint(0, 127, (*shape, D), generator=gen, device="cuda", dtype=torch.uint8)
+            c[name + "_scale"] = torch.rand(shape, generator=gen, device="cuda") / 200
+    c["table"] = torch.randperm(P, generator=gen, device="cuda").to(torch.int32).view(B, 20)
+    if gaps:
+        c["table"][0, 9], c["table"][1, 2], c["table"][1, 10:] = -1, P, -1
+    c["len"] = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    c["pos"] = c["len"] + 10
+    c["parent"] = None
+    c["q"] = torch.randn((B, n, Hq, D), generator=gen, device="cuda").to(torch.bfloat16)
+    want, want_lse, _ = call(c)
+    order = torch.randperm(16 * P, generator=gen, device="cuda")
+    place = torch.empty_like(order)
+    place[order] = torch.arange(16 * P, device="cuda")                      # small page -> where it lies now
+    small = dict(c)
+    for name in ("k", "v", "k_scale", "v_scale"):
+        t = c[name]
+        if t is not None:
+            small[name] = t.view(P, Hkv, 16, 16, -1).transpose(1, 2).reshape(16 * P, Hkv, 16, *t.shape[3:])[order].contiguous()
+    table = c["table"].long()
+    there = (table >= 0) & (table < P)
+    at = place[(table.clamp(0, P - 1)[..., None] * 16 + torch.arange(16, device="cuda")).view(B, -1)]
+    small["table"] = torch.where(there.repeat_interleave(16, 1), at, -1).to(torch.int32)
+    out, lse, _ = call(small)
+    assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    assert torch.isfinite(want.float()).all() and want.abs().sum() > 0
