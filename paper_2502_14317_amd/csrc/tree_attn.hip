@@ -84,6 +84,8 @@ __device__ __forceinline__ uint32_t tree_sight(unsigned long long above, int fir
 struct TreePiece {
   int b, g, row0, n_here;  // query rows row0 .. row0 + n_here - 1 of (node, head)
   int len, base;           // rows that are there, the first of the tree's
+  // blocks in front of this one hold 32 rows that are there, in front of the tree (it may begin behind all that there is room for)
+  __device__ __forceinline__ int whole() const { return max(min(base, len), 0) / 32; }
 };
 
 // A 32-key block: its two halves of 16 keys, each inside a page
@@ -192,7 +194,7 @@ struct TreeWalk {
     end = blk0 + (int)((long long)n_blk * (wave + 1) / TREE_WAVES);
     tab.begin(a, x, (32 * first) >> a.c.pages.shift);
     whole_end = first < end && tab.all(a, x, (32 * first) >> a.c.pages.shift, (min(32 * end, x.len) - 1) >> a.c.pages.shift)
-                    ? min(end, max(x.base, 0) / 32) : first;
+                    ? min(end, x.whole()) : first;
     cur = block(a, x, first);
     keys(a, cur);
     values(a, cur);
@@ -678,7 +680,7 @@ __device__ __forceinline__ void tree_tile_piece(const TreeArgs& a, const TreePie
   // A block has arrived when all but the wavefront's loads of those behind it have, and everybody says so; by then everybody has left
   // the block in front of it, whose place the next one takes.  8 bits: the block behind the one at hand has, to be widened, and the one
   // at hand is.  Blocks that every column sees whole come first, in a loop of their own (none where one of the piece's pages is not there).
-  const int whole_end = all_there ? min(end, max(x.base, 0) / 32) : blk0;
+  const int whole_end = all_there ? min(end, x.whole()) : blk0;
   auto arrive = [&]() __attribute__((always_inline)) {
     TREE_TILE_BARRIER((LAG - (Q8 ? 2 : 1)) * Tiles::LOADS);
     __builtin_amdgcn_sched_barrier(0);
