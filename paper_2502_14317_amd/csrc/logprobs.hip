@@ -1,8 +1,10 @@
-// What the tokens of a vocabulary are worth: one pass over a row of logits x keeps, relative to a running maximum m in log2
-// units, l = sum 2^(x - m) and e = sum 2^(x - m) (x - m), from which with L = log2 l
-//   log2 p(v) = x_v - m - L,   entropy / ln 2 = L - e / l.
-// A term of x = -inf is 0 (where one is met its factor is held above -1e4, and 2^-1e4 is 0); NaN and +inf make l NaN, and with it every number
-// of the row.
+// What the tokens of a vocabulary are worth: one pass over a row of logits x keeps, relative to a running maximum m of them,
+// l = sum exp(x - m) and e = sum exp(x - m) (x - m), from which
+//   log p(v) = x_v - m - log l,   entropy = log l - e / l.
+// m is a logit, and what is multiplied by log2 e for the exponential is the difference: of a logit the product is out of range for the
+// lowest and largest values of either type, and from 2^30 on its rounding alone takes the exponential out of range.
+// A term of x - m = -inf is 0 (where one is met its factor is held above -1e4, and exp(-1e4) is 0); NaN and +inf make l NaN, and with it every
+// number of the row.
 // The n_top largest: the pass knows the largest logit of every thread.  With the j-th largest of those in each of F
 // wavefronts, F j >= n_top, the least of the F is one that n_top logits at least reach, and few more do (20 of 128256: some 70).
 // The threads whose largest reaches it, some F j, have their logits read once more, from the caches; those that reach it
@@ -40,7 +42,7 @@ struct LogSum {
   // relative to `to` >= m instead; where nothing but -inf has been seen l and e are 0, or NaN if a NaN has
   __device__ __forceinline__ void move(float to) {
     if (m != -INFINITY) {
-      const float d = m - to, a = __builtin_amdgcn_exp2f(d);
+      const float d = m - to, a = __builtin_amdgcn_exp2f(d * LOGPROBS_LOG2E);
       e = d == 0.f ? e : a * fmaf(fmaxf(d, -1e4f), l, e);
       l *= a;
     }
@@ -58,23 +60,22 @@ struct LogSum {
   template <int N, bool HELD = false>
   __device__ __forceinline__ float add(const float (&x)[N], float largest) {
     if constexpr (!HELD) {
-      const float top = largest * LOGPROBS_LOG2E;           // (log2 e > 0: the maximum commutes with it)
-      if (__any(top > m)) {
-        if (top > m) move(top);
+      if (__any(largest > m)) {
+        if (largest > m) move(largest);
       }
     }
     const float ref = m == -INFINITY ? 0.f : m;
     float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const float t = fmaf(x[i], LOGPROBS_LOG2E, -ref), p = __builtin_amdgcn_exp2f(t);
+      const float d = x[i] - ref, p = __builtin_amdgcn_exp2f(d * LOGPROBS_LOG2E);
       if constexpr (!HELD) l += p;
-      sum = fmaf(p, HELD ? fmaxf(t, -1e4f) : t, sum);
+      sum = fmaf(p, HELD ? fmaxf(d, -1e4f) : d, sum);
     }
     return sum;
   }
-  __device__ __forceinline__ float logprob(float x) const { return (fmaf(x, LOGPROBS_LOG2E, -m) - log2f(l)) * LOGPROBS_LN2; }
-  __device__ __forceinline__ float entropy() const { return (log2f(l) - e / l) * LOGPROBS_LN2; }
+  __device__ __forceinline__ float logprob(float x) const { return (x - m) - log2f(l) * LOGPROBS_LN2; }
+  __device__ __forceinline__ float entropy() const { return log2f(l) * LOGPROBS_LN2 - e / l; }
 };
 
 struct LogprobsArgs {
