@@ -508,7 +508,8 @@ typedef struct pc_page_cache {
  *   its segments.  A row that holds an infinity or a NaN reads back as NaN from 8 bits.
  *   pos [B] int32 (device), nullable (keys arrive rotated; rope_base is not looked at)
  *   len_in [B] int32 (device), nullable (all 0; at least 0); len_out [B], nullable: len_in + n_rows, whether the rows are
- *   there or not.  They must not overlap (refused): each of a sequence's workgroups reads len_in.
+ *   there or not.  len_out must not overlap len_in, nor, with rows to append, n_rows, pos or parent (refused): each of a
+ *   sequence's workgroups reads those.
  * B * n_new * H_kv < 2^31.  No workspace. */
 int pc_kv_append_paged(const void* k_new, const void* v_new, int64_t batch_stride, int64_t row_stride, int64_t head_stride,
                        const int32_t* parent, const int32_t* n_rows, const int32_t* pos, int32_t pos0, float rope_base,

@@ -11,10 +11,10 @@ static int check_heads(int n_q_heads, int n_kv_heads, int head_dim) {
 static int check_rope(const int32_t* pos, float base) {
   return pos && (!(base > 1.0f) || !isfinite(base)) ? PC_ERR_SHAPE : PC_OK;
 }
-// Do [batch] 32-bit values at a and at b share memory?  (Every workgroup reads lengths that one of them would write.)
-static bool overlap(const int32_t* a, const int32_t* b, int batch) {
+// Do na 32-bit values at a and nb at b share memory?  (Every workgroup reads lengths and trees that one of them would write over.)
+static bool overlap(const int32_t* a, long long na, const int32_t* b, long long nb) {
   const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return a && b && (x < y ? y - x : x - y) < (uintptr_t)batch * 4;
+  return a && b && (x < y ? y - x < (uintptr_t)na * 4 : x - y < (uintptr_t)nb * 4);
 }
 // Strides in elements of rows of whole 16-byte pieces
 static bool strides_fit(int64_t a, int64_t b, int64_t c) {
@@ -56,7 +56,10 @@ extern "C" int pc_kv_append_paged(const void* k_new, const void* v_new, int64_t 
     if (!k_new || !v_new) return PC_ERR_NULL;
     if ((rc = check_page_memory(c.pages, n_kv_heads)) != PC_OK) return rc;
   }
-  if (overlap(len_in, len_out, batch)) return PC_ERR_SHAPE;
+  if (overlap(len_out, batch, len_in, batch)) return PC_ERR_SHAPE;
+  if (n_new > 0 && (overlap(len_out, batch, n_rows, batch) || overlap(len_out, batch, pos, batch) ||
+                    overlap(len_out, batch, parent, (long long)batch * n_new)))
+    return PC_ERR_SHAPE;
   if (!pc_aligned(k_new, 16) || !pc_aligned(v_new, 16)) return PC_ERR_SHAPE;
   for (const void* p : {(const void*)parent, (const void*)n_rows, (const void*)pos, (const void*)len_in, (const void*)len_out})
     if (!pc_aligned(p, 4)) return PC_ERR_SHAPE;
@@ -167,7 +170,7 @@ extern "C" int pc_tree_accept(const int32_t* tokens, const int32_t* parent, cons
     const int rc = check_page_memory(c.pages, n_kv_heads);
     if (rc != PC_OK) return rc;
     if (!len_in) return PC_ERR_NULL;
-    if (overlap(len_in, len_out, batch) || overlap(len_in, pos, batch) || overlap(len_out, pos, batch)) return PC_ERR_SHAPE;
+    if (overlap(len_in, batch, len_out, batch) || overlap(len_in, batch, pos, batch) || overlap(len_out, batch, pos, batch)) return PC_ERR_SHAPE;
     c.moves = 1; c.n_kv_heads = n_kv_heads; c.head_dim = head_dim; c.len_in = len_in; c.len_out = len_out;
   }
   for (const void* p : {(const void*)tokens, (const void*)parent, (const void*)choice, (const void*)n_rows, (const void*)len_in,
