@@ -564,8 +564,8 @@ size_t pc_token_logprobs_workspace_bytes(int32_t rows, int32_t vocab, int32_t n_
  *   cache: rows are moved; NULL: none (n_kv_heads, head_dim, len_in and len_out are not looked at).  A layer's call each; one of
  *     them brings the lengths and positions up to date.
  *   len_in [B] int32 (device): rows with the tree's; len_out [B], nullable: base + n_kept.
- *   pos [B] int32 (device), nullable: n_kept is added in place.  len_in, len_out and pos must not overlap (refused where there is a
- *     cache), and no output an input: each of a sequence's workgroups walks its tree.
+ *   pos [B] int32 (device), nullable: n_kept is added in place.  With a cache len_in, len_out and pos must not overlap, nor, of more
+ *     than one node, any output any input (refused): each of a sequence's workgroups walks its tree.
  * Rows that are not there are not moved.  n 1 .. 64, batch up to 2^20.  No workspace. */
 int pc_tree_accept(const int32_t* tokens, const int32_t* parent, const int32_t* choice, int32_t choice_stride,
                    const int32_t* n_rows, int32_t batch, int32_t n, const pc_page_cache* cache, int32_t n_kv_heads,

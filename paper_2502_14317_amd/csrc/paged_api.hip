@@ -171,6 +171,15 @@ extern "C" int pc_tree_accept(const int32_t* tokens, const int32_t* parent, cons
     if (rc != PC_OK) return rc;
     if (!len_in) return PC_ERR_NULL;
     if (overlap(len_in, batch, len_out, batch) || overlap(len_in, batch, pos, batch) || overlap(len_out, batch, pos, batch)) return PC_ERR_SHAPE;
+    if (n > 1) {                                             // (of one node nothing moves)
+      const long long nodes = (long long)batch * n, choices = (nodes - 1) * choice_stride + 1;
+      for (int32_t* out : {path, n_kept, next_token, len_out, pos}) {
+        const long long m = out == path ? nodes : batch;
+        if (overlap(out, m, tokens, nodes) || overlap(out, m, parent, nodes) || overlap(out, m, choice, choices) || overlap(out, m, n_rows, batch) ||
+            overlap(out, m, len_in, batch))
+          return PC_ERR_SHAPE;
+      }
+    }
     c.moves = 1; c.n_kv_heads = n_kv_heads; c.head_dim = head_dim; c.len_in = len_in; c.len_out = len_out;
   }
   for (const void* p : {(const void*)tokens, (const void*)parent, (const void*)choice, (const void*)n_rows, (const void*)len_in,
