@@ -534,19 +534,26 @@ class PagedTreeDecoder:
             _must_be((n0, self.Hkv, self.D), torch.bfloat16, k_tail=k_tail, v_tail=v_tail)
         if _capturing(self.len):
             raise ValueError("a sequence is loaded outside of graphs")
-        total = sum(lens) + n0
+        b, pos, total = range(self.B)[b], int(pos), sum(lens) + n0
+        if not -2 ** 31 <= pos < 2 ** 31:
+            raise ValueError(f"position {pos} has more than 32 bits")
         self._fits(b, total)
         self._ready(self.table.device)
+        to = lambda x: torch.tensor(x, dtype=torch.int32, device=self.table.device)
+        parts = []                                                          # rows, sequences, rows of each, the first's places, how many are theirs
+        if n_seg and k_t:                                                   # each segment a sequence of its own, behind the one before
+            parts.append((kc.transpose(1, 2), vc.transpose(1, 2), n_seg, k_t, to([sum(lens[:s]) for s in range(n_seg)]), to(lens)))
+        if n0:
+            parts.append((k_tail[None], v_tail[None], 1, n0, to([total - n0]), to([n0])))
+
+        def append(k, v, m, n, first, rows):
+            B.pc_kv_append_paged(k, v, m, n, self.Hkv, self.D, self._cache(self.table[b].repeat(m, 1)), first, None, n_rows=rows)
+        for *part, rows in parts:                                           # none of the rows: refused is what is refused, with the old document in place
+            append(*part, torch.zeros_like(rows))
         self.release(b)
         self.reserve(b, total)
-        i32, device = torch.int32, self.table.device
-        to = lambda x: torch.tensor(x, dtype=i32, device=device)
-        if n_seg and k_t:                                                   # each segment a sequence of its own, behind the one before
-            first = [sum(lens[:s]) for s in range(n_seg)]
-            B.pc_kv_append_paged(kc.transpose(1, 2), vc.transpose(1, 2), n_seg, k_t, self.Hkv, self.D,
-                                 self._cache(self.table[b].repeat(n_seg, 1)), to(first), None, n_rows=to(lens))
-        if n0:
-            B.pc_kv_append_paged(k_tail[None], v_tail[None], 1, n0, self.Hkv, self.D, self._cache(self.table[b:b + 1]), to([total - n0]), None)
+        for part in parts:
+            append(*part)
         self.len[b], self.pos[b] = total, pos
         self.most[b] = total
 
