@@ -449,9 +449,9 @@ class PagedTreeDecoder:
       release(b)      sequence b's pages are free again
     A step that has not been accepted when a sequence is loaded or released is dropped: accept() asks for the next one.
 
-    Lengths and positions live on the device.  The host keeps a bound of each sequence's rows and reads the lengths only where a
-    sequence could pass the end of its pages; then it takes pages for it, and raises if there are none, before anything is
-    written.  A step in a captured graph takes no pages: reserve() them first, and see to it that the rows of the replays fit.
+    Lengths and positions live on the device.  The host keeps a bound of each sequence's rows and reads the lengths, and how many
+    rows a step has of each, only where a sequence could pass the end of its pages with all of the step's; then it takes pages for it,
+    and raises if there are none, before anything is written.  A step in a captured graph takes no pages: reserve() them first, and see to it that the rows of the replays fit.
     Rows behind a sequence's pages are dropped, and nobody sees them."""
 
     def __init__(self, batch, n_pages, page, max_pages, n_q_heads, n_kv_heads, head_dim, rope_base, max_rows=1, softmax_scale=0.0,
@@ -468,6 +468,7 @@ class PagedTreeDecoder:
         self.free = list(range(n_pages - 1, -1, -1))
         self.pages = [None] * batch                                         # of a sequence; None: not loaded
         self.most = [0] * batch                                             # no sequence has more rows that stand
+        self.more = [0] * batch                                             # ... more than this from the step at hand
         self.known = True                                                   # False: graphs move the lengths unseen
         self.at_hand = None                                                 # (rows, parent, n_rows) of the step that is not accepted yet
         self.out = torch.empty((batch, max_rows, n_q_heads, head_dim), dtype=torch.bfloat16, device=device)
@@ -564,21 +565,24 @@ class PagedTreeDecoder:
             raise ValueError(f"sequence {b}: {rows} rows need {need} pages of {self.page}, {len(self.free)} are free, {self.max_pages} a "
                              "sequence at most")
 
-    def _room(self, n):
-        """Pages for n rows more of every sequence."""
+    def _room(self, n, n_rows):
+        """Pages for the step's rows: n of every sequence, or min(n, n_rows[b]) of sequence b, where they are read."""
+        self.more = [n] * self.B
         if _capturing(self.len):
             self.known = False                                              # replays will move the lengths unseen
             return
-        short = lambda: [b for b, p in enumerate(self.pages) if p is not None and self.most[b] + n > len(p) * self.page]
+        short = lambda: [b for b, p in enumerate(self.pages) if p is not None and self.most[b] + self.more[b] > len(p) * self.page]
         if not self.known or short():
             self.most = self.len.tolist()
+            if n_rows is not None:
+                self.more = [min(max(x, 0), n) for x in n_rows.tolist()]
         short = short()
-        need = [(self.most[b] + n + self.page - 1) // self.page for b in short]
+        need = [(self.most[b] + self.more[b] + self.page - 1) // self.page for b in short]
         if any(x > self.max_pages for x in need) or sum(need) - sum(len(self.pages[b]) for b in short) > len(self.free):
-            raise ValueError(f"{n} rows more do not fit: sequences {short} of {[self.most[b] for b in short]} rows, {len(self.free)} pages "
-                             f"of {self.page} are free, {self.max_pages} a sequence at most")
+            raise ValueError(f"{[self.more[b] for b in short]} rows more do not fit: sequences {short} of {[self.most[b] for b in short]} rows, "
+                             f"{len(self.free)} pages of {self.page} are free, {self.max_pages} a sequence at most")
         for b in short:
-            self.reserve(b, self.most[b] + n)
+            self.reserve(b, self.most[b] + self.more[b])
 
     def step(self, q, k, v, parent=None, n_rows=None):
         """q [B, n, H_q, D], k, v [B, n, H_kv, D] bf16 before RoPE, n <= max_rows: the nodes of every sequence's tree; parent
@@ -594,7 +598,7 @@ class PagedTreeDecoder:
                 _must_be(shape, torch.int32, **{name: t})
         if n_rows is None and None in self.pages:
             raise ValueError(f"sequence {self.pages.index(None)} is not loaded: say with n_rows who takes part")
-        self._room(n)
+        self._room(n, n_rows)
         self._ready(q.device)
         B.pc_kv_append_paged(k, v, self.B, n, self.Hkv, self.D, self.cache, self.len, self.len_new, pos=self.pos,
                              rope_base=self.rope_base, parent=parent, n_rows=n_rows)
@@ -617,5 +621,5 @@ class PagedTreeDecoder:
                          cache=self.cache, n_kv_heads=self.Hkv, head_dim=self.D, len_in=self.len_new, len_out=self.len, pos=self.pos,
                          n_rows=n_rows)
         self.at_hand = None
-        self.most = [m + n for m in self.most]
+        self.most = [m + x for m, x in zip(self.most, self.more)]
         return path, self.n_kept, self.next_token
