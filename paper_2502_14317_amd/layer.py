@@ -451,7 +451,9 @@ class PagedTreeDecoder:
 
     Lengths and positions live on the device.  The host keeps a bound of each sequence's rows and reads the lengths, and how many
     rows a step has of each, only where a sequence could pass the end of its pages with all of the step's; then it takes pages for it,
-    and raises if there are none, before anything is written.  A step in a captured graph takes no pages: reserve() them first, and see to it that the rows of the replays fit.
+    and raises if there are none, before anything is written.  A step in a captured graph takes no pages: reserve() them first,
+    and see to it that the rows of the replays fit.  It is accepted in a graph, too, its own or one that is captured next and
+    replayed behind it: the host does not see replays.
     Rows behind a sequence's pages are dropped, and nobody sees them."""
 
     def __init__(self, batch, n_pages, page, max_pages, n_q_heads, n_kv_heads, head_dim, rope_base, max_rows=1, softmax_scale=0.0,
@@ -470,7 +472,7 @@ class PagedTreeDecoder:
         self.most = [0] * batch                                             # no sequence has more rows that stand
         self.more = [0] * batch                                             # ... more than this from the step at hand
         self.known = True                                                   # False: graphs move the lengths unseen
-        self.at_hand = None                                                 # (rows, parent, n_rows) of the step that is not accepted yet
+        self.at_hand = None                                                 # (rows, parent, n_rows, captured) of the step that is not accepted yet
         self.out = torch.empty((batch, max_rows, n_q_heads, head_dim), dtype=torch.bfloat16, device=device)
         self.lse = torch.empty((batch, n_q_heads, max_rows), dtype=torch.float32, device=device)
         self.path = torch.empty((batch, max_rows), dtype=i32, device=device)
@@ -606,7 +608,7 @@ class PagedTreeDecoder:
         lse = self.lse.view(-1)[:self.B * self.Hq * n].view(self.B, self.Hq, n)
         B.pc_tree_attn(q, self.cache, self.len_new, self.B, n, self.Hq, self.Hkv, self.D, out, lse, self.ws, parent=parent, n_rows=n_rows,
                        pos=self.pos, rope_base=self.rope_base, softmax_scale=self.scale)
-        self.at_hand = (n, parent, n_rows)
+        self.at_hand = (n, parent, n_rows, _capturing(self.len))
         return out
 
     def accept(self, tokens, choice, choice_stride=1):
@@ -614,7 +616,9 @@ class PagedTreeDecoder:
         Returns path [B, n], n_kept [B], next_token [B] (views of the decoder's buffers)."""
         if self.at_hand is None:
             raise ValueError("no step at hand")
-        n, parent, n_rows = self.at_hand
+        n, parent, n_rows, captured = self.at_hand
+        if captured != _capturing(self.len):
+            raise ValueError("a step in a graph is accepted in a graph, another one outside")
         _must_be((self.B, n), torch.int32, tokens=tokens)
         path = self.path.view(-1)[:self.B * n].view(self.B, n)
         B.pc_tree_accept(tokens, parent, choice, self.B, n, path, self.n_kept, self.next_token, choice_stride=choice_stride,

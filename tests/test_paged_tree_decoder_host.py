@@ -132,3 +132,41 @@ def test_sequences_that_are_not_loaded_take_no_pages(lib):
         step(d, 4, [4, 0])
         accept(d, 4)
     assert d.len.tolist() == [62, 0] and d.pages[1] is None
+
+
+def test_steps_and_acceptances_are_captured_together(lib, monkeypatch):
+    """The host does not see replays: an acceptance outside would be one for all of them, and one inside would move lengths unseen."""
+    d = decoder([20, 20])
+    capture = lambda on: monkeypatch.setattr(layer, "_capturing", lambda t: on)
+    capture(True)
+    step(d, 3)
+    capture(False)
+    for _ in range(2):
+        lib.calls.clear()
+        with pytest.raises(ValueError, match="graph"):
+            accept(d, 3)
+        assert lib.calls == []
+    capture(True)
+    accept(d, 3)                                                            # in a graph behind it
+    capture(False)
+    with pytest.raises(ValueError, match="no step"):
+        accept(d, 3)
+    before = d.len.tolist()
+    step(d, 2)
+    capture(True)
+    lib.calls.clear()
+    with pytest.raises(ValueError, match="graph"):
+        accept(d, 2)
+    assert lib.calls == []
+    capture(False)
+    accept(d, 2)                                                            # the step is still at hand
+    assert d.len.tolist() == [x + 2 for x in before]
+    capture(True)
+    step(d, 4)
+    capture(False)
+    step(d, 1)                                                              # an eager step counts for itself
+    accept(d, 1)
+    assert d.len.tolist() == [x + 3 for x in before]
+    d.len.fill_(47)                                                         # what replays leave behind
+    step(d, 4)
+    assert d.most == [47, 47] and [len(p) for p in d.pages] == [4, 4]
