@@ -469,14 +469,20 @@ __global__ __launch_bounds__(JOIN_THREADS) void logprobs_join_kernel(LogprobsArg
 //   bf16 (16 x 32000) 8.4 / 11.4   (16 x 64000) 9.8 / 11.6   (4 x 128256) 13.3 / 11.8   (64 x 128256) 14.0 / 13.2   (128 x 128256) 15.0 / 15.5
 //   fp32 (16 x 32000) 7.9 / 10.7   (64 x 64000) 10.2 / 11.8  (4 x 128256) 14.0 / 11.2   (64 x 128256) 17.4 / 13.9   (128 x 128256) 18.3 / 19.6
 // Threads of a workgroup, 256 / 512 / 1024: (512 x 128256 fp32, 20) 65.9 / 58.4 / 57.5, (2048 x 128256 bf16, 5) 103.6 / 100 / 110.8.
+#define LOGPROBS_WHOLE (192 * 1024)
+#define LOGPROBS_PARTS 256
+#define LOGPROBS_PART 16384
 static int logprobs_parts(int rows, int vocab, int fp32) {
   const long long bytes = (long long)vocab * (fp32 ? 4 : 2);
-  const int parts = 256 / (rows < 1 ? 1 : rows), most = (int)(bytes / 16384);
-  if (bytes <= 192 * 1024 || parts < 4) return 1;
+  const int parts = LOGPROBS_PARTS / (rows < 1 ? 1 : rows), most = (int)(bytes / LOGPROBS_PART);
+  if (bytes <= LOGPROBS_WHOLE || parts < 4) return 1;
   return parts < most ? parts : most;
 }
+// Rows in one part use none: room for the 256 parts that fewer rows are cut into, or as many as they could have (of either type: 32 bits
+// have as many or more)
 size_t pc_logprobs_ws_bytes(int rows, int vocab, int n_top) {
-  const size_t n = (size_t)rows * logprobs_parts(rows, vocab, 1);        // (of either type: 32 bits have as many parts or more)
+  const long long bytes = (long long)vocab * 4, most = bytes > LOGPROBS_WHOLE ? rows * (bytes / LOGPROBS_PART) : 0;
+  const size_t n = (size_t)(most < LOGPROBS_PARTS ? most : LOGPROBS_PARTS);
   return pc_align_up(n * sizeof(LogSum), 256) + pc_align_up(n * n_top * sizeof(top_key), 256) + 256;
 }
 
@@ -498,7 +504,7 @@ int pc_launch_logprobs(const PcLogprobs& c, void* ws, hipStream_t st) {
   a.c = c;
   a.parts = logprobs_parts(c.rows, c.vocab, c.fp32);
   a.parts_div = pc_div_by(a.parts);
-  a.sums = (LogSum*)ws;
+  a.sums = (LogSum*)ws;                                     // (of rows in several parts)
   a.tops = (top_key*)((char*)ws + pc_align_up((size_t)c.rows * a.parts * sizeof(LogSum), 256));
   return c.fp32 ? launch<float>(a, st) : launch<uint16_t>(a, st);
 }
