@@ -512,10 +512,10 @@ class PagedTreeDecoder:
         """Sequence b has ended."""
         if _capturing(self.len):
             raise ValueError("a sequence ends outside of graphs")
-        self.at_hand = None                                                 # (its lengths are another sequence's now)
-        if self.pages[b] is None:
+        pages, self.at_hand = self.pages[b], None                           # (its lengths are another sequence's now)
+        if pages is None:
             return
-        self.free += reversed(self.pages[b])
+        self.free += reversed(pages)
         self.pages[b], self.most[b] = None, 0
         self.table[b].fill_(-1)
         self.len[b], self.pos[b] = 0, 0

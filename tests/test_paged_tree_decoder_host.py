@@ -170,3 +170,12 @@ def test_steps_and_acceptances_are_captured_together(lib, monkeypatch):
     d.len.fill_(47)                                                         # what replays leave behind
     step(d, 4)
     assert d.most == [47, 47] and [len(p) for p in d.pages] == [4, 4]
+
+
+def test_a_release_of_no_sequence_keeps_the_step_at_hand(lib):
+    d = decoder([20, 20])
+    step(d, 2)
+    with pytest.raises(IndexError):
+        d.release(2)
+    accept(d, 2)
+    assert d.len.tolist() == [22, 22]
