@@ -528,7 +528,7 @@ int pc_kv_append_paged(const void* k_new, const void* v_new, int64_t batch_strid
  * Arithmetic as pc_shared_attn's: bf16 MFMA products (8-bit codes widened exactly), logits, softmax and sums in fp32,
  * probabilities (at most 1; times the row's V scale) rounded to bf16 once.  The way a sequence's rows are cut, and with
  * it the last bits of its result, depends on the lengths of the whole batch; the same call gives the same bits.
- * H_q up to 2^20, batch up to 2^20, B n H_q < 2^25, B max_pages page < 2^36.  Workspace: pc_tree_attn_workspace_bytes(...) of
+ * H_q up to 2^20, batch 1 up to 2^20, B n H_q < 2^25, B max_pages page < 2^36.  Workspace: pc_tree_attn_workspace_bytes(...) of
  * the same sizes: it does not depend on lengths, so that a captured call stays valid as they grow. */
 int pc_tree_attn(const void* q, int64_t batch_stride, int64_t row_stride, const int32_t* parent, const int32_t* n_rows,
                  const int32_t* pos, int32_t pos0, float rope_base, float softmax_scale, const pc_page_cache* cache,

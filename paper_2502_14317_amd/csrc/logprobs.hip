@@ -390,7 +390,9 @@ __global__ __launch_bounds__(LOGPROBS_THREADS) void logprobs_rows_kernel(Logprob
       for (int e = 0; e < VE; e += 2) top = fmaxf(fmaxf(top, x[u * VE + e]), x[u * VE + e + 1]);
     }
     float terms = s.add(x, top);
-    if (__any(terms != terms)) {                            // a logit of -inf, or worse: once more, from the caches
+    // A logit of -inf, or worse, or a difference of that: once more, from the caches.  Pieces behind the row's end are -inf, so this is also
+    // every row's last round, unless its pieces are a multiple of the round's 2048: an eighth of 128256 16-bit logits, half of 32000.
+    if (__any(terms != terms)) {
       terms = 0.f;
 #pragma unroll 1
       for (int i = i0; i < min(i0 + U * LOGPROBS_THREADS, r.hi); i += LOGPROBS_THREADS) {
@@ -466,9 +468,10 @@ __global__ __launch_bounds__(JOIN_THREADS) void logprobs_join_kernel(LogprobsArg
 // ---- host
 // Workgroups a row: one, in one launch, but for few rows of more than 192 KB, which are cut into about 256 parts in all, of 16 KB at
 // least.  us a call, one / 256 parts in all, 5 of the largest asked for:
-//   bf16 (16 x 32000) 8.4 / 11.4   (16 x 64000) 9.8 / 11.6   (4 x 128256) 13.3 / 11.8   (64 x 128256) 14.0 / 13.2   (128 x 128256) 15.0 / 15.5
-//   fp32 (16 x 32000) 7.9 / 10.7   (64 x 64000) 10.2 / 11.8  (4 x 128256) 14.0 / 11.2   (64 x 128256) 17.4 / 13.9   (128 x 128256) 18.3 / 19.6
-// Threads of a workgroup, 256 / 512 / 1024: (512 x 128256 fp32, 20) 65.9 / 58.4 / 57.5, (2048 x 128256 bf16, 5) 103.6 / 100 / 110.8.
+//   bf16 (16 x 32000) 8.7 / 12.3   (16 x 64000) 10.6 / 12.2   (64 x 64000) 10.9 / 12.9   (4 x 128256) 14.5 / 12.2   (64 x 128256) 15.6 / 14.6   (128 x 128256) 16.4 / 17.3
+//   fp32 (16 x 32000) 8.4 / 11.2   (16 x 64000) 10.7 / 11.6   (64 x 64000) 12.3 / 13.2   (4 x 128256) 15.1 / 11.7   (64 x 128256) 18.3 / 16.0   (128 x 128256) 19.2 / 20.3
+// (16 and 64 rows of 250 KB are cut by this and lose 1 us.)
+// Threads of a workgroup, 256 / 512 / 1024: (16 x 32000 bf16, 1) 8.4 / 8.3 / 10.1, (512 x 128256 fp32, 20) 64 / 57 / 55, (2048 x 128256 bf16, 5) 104 / 100 / 109.
 #define LOGPROBS_WHOLE (192 * 1024)
 #define LOGPROBS_PARTS 256
 #define LOGPROBS_PART 16384

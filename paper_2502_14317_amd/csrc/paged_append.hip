@@ -2,10 +2,13 @@
 // are written (bf16, or E4M3 with a scale a row).  A row is 16 lanes' of D / 16 consecutive values each; lane m turns its
 // values with lane m ^ 8's, and each computes half of their common angles.
 // A token's angles are its KV heads' alike: with many rows 16 lanes take up to 8 heads of a token one after the other (each head with
-// its own angles, whose 64-bit arithmetic was the bound: 8 x 8192 tokens of 8 heads of 128 values to 8 bits 108 us, with 2 / 4 / 8 heads
-// 88 / 82 / 77); four tokens of a wavefront lie behind each other in a page.
-// Bound by memory for prompts (those 77 us are 5.3 TB/s, to 16 bits 108 us = 5.0, a large copy 5.1), by a launch's latency for a
-// step.  Stores past the caches: 83 us instead of 77, to 16 bits 106 instead of 108, with 64 values 54 instead of 45.
+// its own angles, whose 64-bit arithmetic was the bound); four tokens of a wavefront lie behind each other in a page.  us for 8 x 8192
+// tokens of 8 heads, 1 / 2 / 4 / 8 heads one after the other:
+//   128 values to 8 bits  106 / 88 / 88 / 88, the same input again and again 102 / 79 / 72 / 73      64 values to 8 bits  72 / 53 / 46 / 44
+//   128 values to 16 bits 112 / 108 / 109 / 110 (95 / 81 / 81 / 81)
+// Bound by memory for prompts (inputs that change: 87 us = 4.7 TB/s, to 16 bits 110 us = 4.9, a large copy 5.1), by a launch's latency for
+// a step.  Stores past the caches: 81 us instead of 88 and 106 instead of 111, but with inputs from the caches 80 instead of 73 and 105
+// instead of 81, and 45 instead of 43 with 64 values.
 #include "paged.h"
 #include "row8.h"
 #include "serve.h"

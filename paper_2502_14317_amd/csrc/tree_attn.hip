@@ -14,7 +14,7 @@
 // Bodies: up to 32 rows a wavefront takes a part of the keys, straight into registers; more rows share keys in LDS.
 // Bound (4 D R flops against 4 D bytes a key for R query rows a KV head, 2 D + 8 in 8 bits): memory up to 64 rows, 32 sequences of
 // 8300 rows on average, 4 query rows a KV head, 8 KV heads of 128 values 167 us = 6.5 TB/s; 16 sequences of 11500 rows, 64 query
-// rows 138 us = 5.5 TB/s; with 128 rows, 8 sequences of 46000 rows in 8 bits 328 us = 0.59 PFLOP/s, 0.89 with the products of the
+// rows 138 us = 5.5 TB/s; with 128 rows, 8 sequences of 46000 rows in 8 bits some 330 us = 0.59 PFLOP/s, 0.89 with the products of the
 // rotated queries' second parts: a block's chain of a barrier, scalar instructions, reads of LDS, products and softmax, of which
 // two wavefronts a SIMD hide a part of each other's (what was taken off the chain gained, what was taken off the counts did not).
 #include <type_traits>
@@ -384,8 +384,9 @@ __device__ __forceinline__ void tree_piece(const TreeArgs& a, const TreePiece& x
 // have 16 NC query rows each.  8 bits: the workgroup widens a block once, a block ahead of the products (each wavefront for itself,
 // with 48 conversions and 16 permutations more a block: 128 rows 113 us instead of 110, rows of 64 values 104 instead of 102, 64 rows of
 // 128 values 150 instead of 154).  A row of 16 bits is PPR
-// pieces of 16 bytes, piece p of row r in place p ^ swizzle(r): so the matrix operands (16 rows at once, or four whole ones) come
-// without bank conflicts, and a load instruction brings whole rows.
+// pieces of 16 bytes, piece p of row r in place p ^ swizzle(r), and a load instruction brings whole rows.  With 128 values the operands of
+// the keys (16 rows at once) come without bank conflicts, those of the values, transposed on the way (eight rows of 32 bytes at once), two
+// to a bank; with 64 values the other way round.  Conflicts are a third of the LDS's busy cycles with 128 values.
 // (Keys straight into registers, two wavefronts to a key, keep half as many bytes on their way: 16 sequences of 11000 rows, 64
 // query rows a KV head, 188 us instead of 140.  32 rows a wavefront, two blocks at a time: 1 to 10 us slower.)
 template <int D, bool Q8>
@@ -886,17 +887,23 @@ PcTreePlan pc_tree_plan(const PcTreeCall& c) {
   const int rows = c.n * (c.n_q_heads / c.n_kv_heads);
   const long long cap = (long long)c.pages.max_pages << c.pages.shift, blocks = c.batch * ((cap + 31) / 32);
   // 17 to 32 rows: the body of 64 keeps more of the longest rows on their way, though it leaves half of its own empty.  us a call,
-  // 32 query rows a KV head, 8 KV heads, sequences x places, body of 32 / of 64:
-  //   bf16, 128 values  (2 x 512) 16 / 20   (2 x 8192) 35 / 29   (16 x 512) 18 / 23   (16 x 2048) 40 / 32   (16 x 4096) 57 / 44   (64 x 8192) 275 / 254
-  //   bf16, 64 values   (16 x 4096) 32 / 32   (16 x 16384) 73 / 83   (64 x 8192) 128 / 150
+  // 32 query rows a KV head, 8 KV heads, sequences x places (and a page), body of 32 / of 64:
+  //   bf16, 128 values    (2 x 512) 15 / 17   (2 x 8192) 37 / 27   (16 x 512) 18 / 17   (16 x 2048) 41 / 29   (16 x 4096) 58 / 44   (64 x 8192) 275 / 255
+  //   bf16, 64 values     (2 x 512) 11 / 14   (2 x 8192) 25 / 23   (16 x 512) 12 / 14   (16 x 2048) 26 / 23   (16 x 4096) 32 / 30   (64 x 8192) 130 / 129
+  //   8 bits, 128 values  (2 x 512) 15 / 20   (2 x 8192) 31 / 30   (16 x 512) 16 / 21   (16 x 2048) 36 / 33   (16 x 4096) 43 / 46   (64 x 8192) 167 / 239
+  //   8 bits, 64 values   (2 x 512) 11 / 15   (2 x 8192) 24 / 24   (16 x 512) 12 / 15   (16 x 2048) 25 / 25   (16 x 4096) 29 / 34   (64 x 8192) 90 / 152
+  // (Shorter rows than the longest take the body of 32 throughout: where that of 64 is ahead, it is by 10 % at most.)
   const bool longest = !c.pages.k_scale && c.head_dim == 128 && cap > 1024;
   p.rows = rows <= 16 ? 16 : (rows <= 32 && !longest ? 32 : (rows <= 64 ? 64 : 128));
   p.tiles = (rows + p.rows - 1) / p.rows;
   // One launch, a workgroup a sequence (and KV head and tile), where the pages hold little for each, or workgroups are many.  us a
   // call, cut / whole, lengths from a third of the pages' on, 8 KV heads of 128 values, sequences x query rows a KV head x places:
-  //   bf16 (2 x 4 x 512) 16.3 / 11.2   (2 x 4 x 1024) 14.3 / 15.1   (16 x 4 x 1024) 21.4 / 20.3   (64 x 4 x 2048) 66.4 / 63.6
-  //   (2 x 64 x 512) 21.4 / 20.5   (16 x 64 x 1024) 30.2 / 33.5   (64 x 64 x 2048) 89 / 75   (64 x 128 x 2048) 134 / 116   (16 x 4 x 2048) 27 / 34
-  //   8 bits (2 x 4 x 1024) 14.0 / 13.7   (16 x 4 x 2048) 21.8 / 22.0   (16 x 128 x 512) 46 / 35   (64 x 128 x 2048) 138 / 117
+  //   bf16 (2 x 4 x 576) 15.5 / 10.5   (2 x 4 x 1024) 14.0 / 18.6   (16 x 4 x 1024) 21.4 / 19.7   (64 x 4 x 2048) 63.7 / 60.4   (16 x 4 x 2048) 26.0 / 33.6
+  //   (2 x 64 x 512) 19.2 / 16.4   (16 x 64 x 1024) 29.0 / 26.9   (64 x 64 x 2048) 86.5 / 68.7   (64 x 128 x 2048) 125 / 96
+  //   8 bits (2 x 4 x 1024) 13.0 / 13.8   (16 x 4 x 1024) 19.5 / 14.5   (16 x 4 x 2048) 21.7 / 21.7   (16 x 128 x 512) 35 / 27   (64 x 128 x 2048) 126 / 102
+  // One rule for both formats and all numbers of sequences, by the pages alone: two sequences of 1024 places lose up to 5 us by it, sixteen gain 2 to 5;
+  // sixteen of 1024 places and 64 rows a KV head would gain 2.  Lengths are not known here, so short sequences in wide tables are cut: up to
+  // 512 rows in tables of 131072 places, 16 sequences x 4 rows, 19.2 us, whole 13.3; x 64 rows 28.3, whole 18.9.
   const long long groups = (long long)c.batch * c.n_kv_heads * p.tiles;
   if ((cap <= (rows <= 32 ? 1024 : 512) || (cap <= 2048 && groups >= 512)) && groups < TREE_GROUPS) {
     p.shares = 0;

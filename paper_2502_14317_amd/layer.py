@@ -523,7 +523,8 @@ class PagedTreeDecoder:
     def load(self, b, kc, vc, pos, seg_len=None, k_tail=None, v_tail=None):
         """kc, vc [n_seg, H_kv, k_t, D] bf16: the document's compacted segments (keys rotated), as the gather leaves them, of
         seg_len[s] rows (None: k_t) each; k_tail, v_tail [n0, H_kv, D] rotated rows of the query block behind them, or None;
-        pos: the position of the sequence's next row.  What sequence b held before is released."""
+        pos: the position of the sequence's next row.  What sequence b held before is released; a load that is refused leaves it.
+        All of a segment's heads have the same rows: one whose heads kept different numbers is not taken."""
         n_seg, _, k_t, _ = kc.shape if kc.dim() == 4 else (0, 0, 0, 0)
         if kc.shape != (n_seg, self.Hkv, k_t, self.D) or kc.shape != vc.shape or kc.dtype != torch.bfloat16 or vc.dtype != kc.dtype:
             raise ValueError(f"kc {tuple(kc.shape)}, vc {tuple(vc.shape)}: not bfloat16 [n_seg, {self.Hkv}, k_t, {self.D}]")
