@@ -470,9 +470,8 @@ class PagedTreeDecoder:
         self.free = list(range(n_pages - 1, -1, -1))
         self.pages = [None] * batch                                         # of a sequence; None: not loaded
         self.most = [0] * batch                                             # no sequence has more rows that stand
-        self.more = [0] * batch                                             # ... more than this from the step at hand
         self.known = True                                                   # False: graphs move the lengths unseen
-        self.at_hand = None                                                 # (rows, parent, n_rows, captured) of the step that is not accepted yet
+        self.at_hand = None                                                 # (rows, parent, n_rows, rows at most, captured) of the step that is not accepted yet
         self.out = torch.empty((batch, max_rows, n_q_heads, head_dim), dtype=torch.bfloat16, device=device)
         self.lse = torch.empty((batch, n_q_heads, max_rows), dtype=torch.float32, device=device)
         self.path = torch.empty((batch, max_rows), dtype=i32, device=device)
@@ -569,23 +568,24 @@ class PagedTreeDecoder:
                              "sequence at most")
 
     def _room(self, n, n_rows):
-        """Pages for the step's rows: n of every sequence, or min(n, n_rows[b]) of sequence b, where they are read."""
-        self.more = [n] * self.B
+        """Pages for the step's rows: n of every sequence, or min(n, n_rows[b]) of sequence b, where they are read.  Returns how many those are."""
+        more = [n] * self.B
         if _capturing(self.len):
             self.known = False                                              # replays will move the lengths unseen
-            return
-        short = lambda: [b for b, p in enumerate(self.pages) if p is not None and self.most[b] + self.more[b] > len(p) * self.page]
+            return more
+        short = lambda: [b for b, p in enumerate(self.pages) if p is not None and self.most[b] + more[b] > len(p) * self.page]
         if not self.known or short():
             self.most = self.len.tolist()
             if n_rows is not None:
-                self.more = [min(max(x, 0), n) for x in n_rows.tolist()]
+                more[:] = [min(max(x, 0), n) for x in n_rows.tolist()]
         short = short()
-        need = [(self.most[b] + self.more[b] + self.page - 1) // self.page for b in short]
+        need = [(self.most[b] + more[b] + self.page - 1) // self.page for b in short]
         if any(x > self.max_pages for x in need) or sum(need) - sum(len(self.pages[b]) for b in short) > len(self.free):
-            raise ValueError(f"{[self.more[b] for b in short]} rows more do not fit: sequences {short} of {[self.most[b] for b in short]} rows, "
+            raise ValueError(f"{[more[b] for b in short]} rows more do not fit: sequences {short} of {[self.most[b] for b in short]} rows, "
                              f"{len(self.free)} pages of {self.page} are free, {self.max_pages} a sequence at most")
         for b in short:
-            self.reserve(b, self.most[b] + self.more[b])
+            self.reserve(b, self.most[b] + more[b])
+        return more
 
     def step(self, q, k, v, parent=None, n_rows=None):
         """q [B, n, H_q, D], k, v [B, n, H_kv, D] bf16 before RoPE, n <= max_rows: the nodes of every sequence's tree; parent
@@ -601,7 +601,7 @@ class PagedTreeDecoder:
                 _must_be(shape, torch.int32, **{name: t})
         if n_rows is None and None in self.pages:
             raise ValueError(f"sequence {self.pages.index(None)} is not loaded: say with n_rows who takes part")
-        self._room(n, n_rows)
+        more = self._room(n, n_rows)
         self._ready(q.device)
         B.pc_kv_append_paged(k, v, self.B, n, self.Hkv, self.D, self.cache, self.len, self.len_new, pos=self.pos,
                              rope_base=self.rope_base, parent=parent, n_rows=n_rows)
@@ -609,7 +609,7 @@ class PagedTreeDecoder:
         lse = self.lse.view(-1)[:self.B * self.Hq * n].view(self.B, self.Hq, n)
         B.pc_tree_attn(q, self.cache, self.len_new, self.B, n, self.Hq, self.Hkv, self.D, out, lse, self.ws, parent=parent, n_rows=n_rows,
                        pos=self.pos, rope_base=self.rope_base, softmax_scale=self.scale)
-        self.at_hand = (n, parent, n_rows, _capturing(self.len))
+        self.at_hand = (n, parent, n_rows, more, _capturing(self.len))
         return out
 
     def accept(self, tokens, choice, choice_stride=1):
@@ -617,7 +617,7 @@ class PagedTreeDecoder:
         Returns path [B, n], n_kept [B], next_token [B] (views of the decoder's buffers)."""
         if self.at_hand is None:
             raise ValueError("no step at hand")
-        n, parent, n_rows, captured = self.at_hand
+        n, parent, n_rows, more, captured = self.at_hand
         if captured != _capturing(self.len):
             raise ValueError("a step in a graph is accepted in a graph, another one outside")
         _must_be((self.B, n), torch.int32, tokens=tokens)
@@ -626,5 +626,5 @@ class PagedTreeDecoder:
                          cache=self.cache, n_kv_heads=self.Hkv, head_dim=self.D, len_in=self.len_new, len_out=self.len, pos=self.pos,
                          n_rows=n_rows)
         self.at_hand = None
-        self.most = [m + x for m, x in zip(self.most, self.more)]
+        self.most = [m + x for m, x in zip(self.most, more)]
         return path, self.n_kept, self.next_token

@@ -179,3 +179,16 @@ def test_a_release_of_no_sequence_keeps_the_step_at_hand(lib):
         d.release(2)
     accept(d, 2)
     assert d.len.tolist() == [22, 22]
+
+
+def test_a_refused_step_leaves_the_bound_of_the_one_at_hand(lib):
+    d = decoder([20, 63])
+    step(d, 4, [4, 1])
+    with pytest.raises(ValueError, match="do not fit"):
+        step(d, 2, [1, 2])
+    accept(d, 4)
+    assert d.len.tolist() == [24, 64] and all(m >= x for m, x in zip(d.most, d.len.tolist()))
+    for _ in range(3):                                                      # 36 rows: a third page
+        step(d, 4, [4, 0])
+        accept(d, 4)
+    assert d.len.tolist() == [36, 64] and len(d.pages[0]) == 3
