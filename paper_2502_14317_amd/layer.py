@@ -605,6 +605,7 @@ class PagedTreeDecoder:
         self._ready(q.device)
         B.pc_kv_append_paged(k, v, self.B, n, self.Hkv, self.D, self.cache, self.len, self.len_new, pos=self.pos,
                              rope_base=self.rope_base, parent=parent, n_rows=n_rows)
+        self.at_hand = None                                                 # (the rows of the step before are written over)
         out = self.out.view(-1)[:q.numel()].view(q.shape)
         lse = self.lse.view(-1)[:self.B * self.Hq * n].view(self.B, self.Hq, n)
         B.pc_tree_attn(q, self.cache, self.len_new, self.B, n, self.Hq, self.Hkv, self.D, out, lse, self.ws, parent=parent, n_rows=n_rows,

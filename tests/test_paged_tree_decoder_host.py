@@ -192,3 +192,27 @@ def test_a_refused_step_leaves_the_bound_of_the_one_at_hand(lib):
         step(d, 4, [4, 0])
         accept(d, 4)
     assert d.len.tolist() == [36, 64] and len(d.pages[0]) == 3
+
+
+def test_a_step_whose_rows_are_written_over_is_no_longer_at_hand(lib, monkeypatch):
+    """An attention that is refused has its append in front of it; an append that is refused has written nothing."""
+    d = decoder([20, 20])
+    step(d, 2)
+    with monkeypatch.context() as m:
+        def refuse(*args, **more):
+            raise ValueError("refused")
+        m.setattr(lib, "pc_kv_append_paged", refuse)
+        with pytest.raises(ValueError, match="refused"):
+            step(d, 4)
+    accept(d, 2)
+    assert d.len.tolist() == [22, 22]
+    step(d, 2)
+    with monkeypatch.context() as m:
+        m.setattr(lib, "pc_tree_attn", refuse)
+        with pytest.raises(ValueError, match="refused"):
+            step(d, 4)
+    with pytest.raises(ValueError, match="no step"):
+        accept(d, 2)
+    step(d, 3)
+    accept(d, 3)
+    assert d.len.tolist() == [25, 25] and all(m >= x for m, x in zip(d.most, d.len.tolist()))
